@@ -328,6 +328,88 @@ vc_status vc_test_nvfp4_codes(const float *s, const float *m, int64_t rows, int3
 vc_status vc_mma_peak(int32_t kind, int32_t groups, void *scratch, double *tflops, double *mac_per_clk_sm,
                       void *stream);
 
+/* ======================================================================================
+ * The rest of an attention layer, at the model's own precision: the norm and rotation of Q and K in
+ * front of vc_attn, attention to an encoder's states, and the E4M3 matrix product of the
+ * projections on either side.  A layer runs
+ *
+ *   vc_quant_fp8 -> vc_linear_fp8 (Q, K, V) -> vc_qk_norm_rope -> vc_attn without VC_FLAG_ROPE
+ *                -> vc_quant_fp8 -> vc_linear_fp8 (output)
+ *
+ * and vc_cross_attn in the place of vc_attn where keys and values come from an encoder.  The paper treats
+ * the quantized self-attention alone; these entry points exist for its callers.  Forward only, as
+ * everything here.  The conventions at the top of this file hold; element types and strides are arguments.
+ * ====================================================================================== */
+enum { VC_DTYPE_BF16 = 0, VC_DTYPE_FP16 = 1, VC_DTYPE_FP32 = 2 };
+
+/* Strides of a [B][H][N][d] tensor in elements, d contiguous; all 0 = packed.  Every row must start on a 16-byte
+ * boundary: the base pointer does, and each stride is a multiple of 16 bytes (a stride of 0 beside others that
+ * are not is a broadcast, for inputs only). */
+typedef struct { int64_t b, h, n; } vc_strides;
+
+/* Norm of queries and keys and their position rotation, in one pass over both.
+ *
+ *   y = x * rsqrt(mean(x^2) + eps) * weight        the mean over one head's channels (VC_NORM_HEAD, weight [d]) or
+ *                                                  over all heads of a token (VC_NORM_TOKEN, weight [H][d])
+ *   (a, b) -> m (a cos t - b sin t, a sin t + b cos t)      t = position * frequency, for every pair (a, b) of channels
+ *
+ * computed in FP32 (the angle in FP64) and rounded once.  The rotated channels are the first
+ * rope_dim_t + rope_dim_h + rope_dim_w of a head, in this order, one position axis each; the others
+ * pass through.  Pair i of an axis with n channels from channel s on is (s + 2 i, s + 2 i + 1)
+ * (VC_ROTARY_INTERLEAVED, what VC_FLAG_ROPE does) or (s + i, s + n / 2 + i) (VC_ROTARY_HALF), and its frequency is
+ * f_i = theta^(-2 i / n), which the axis's factor F = rope_factor_* > 0 (0 => 1) changes for long contexts:
+ *   VC_ROPE_SCALING_LINEAR   f_i / F
+ *   VC_ROPE_SCALING_NTK      theta F^(n / (n - 2)) in the place of theta
+ *   VC_ROPE_SCALING_YARN     f_i (1 - r_i) + f_i / F r_i,  r_i = clamp((i - lo) / (hi - lo), 0, 1) from
+ *                            lo = max(floor(c(beta_fast)), 0), hi = min(ceil(c(beta_slow)), n - 1) (lo + 0.001 where that
+ *                            does not exceed lo), c(b) = n ln(L / (2 pi b)) / (2 ln theta), L = rope_original_* >= 1 the
+ *                            positions the model was trained on
+ * m = rope_attention_factor; 0 => 0.1 ln(largest F of a rotated axis) + 1 with YARN if that F is above 1, else 1.
+ *
+ * Token n sits at (start_t + n / (grid_h grid_w), start_h + n / grid_w % grid_h, start_w + n % grid_w), or, with
+ * `positions` (int32 [B][N][3]), at the three numbers given there (the grid is then not looked at).
+ * Q has H_q heads and K has H_k; 0 heads: the tensor is absent.  q_out / k_out may be q / k themselves with the
+ * same strides, and must not overlap anything else the call reads.  A weight may be NULL (ones). */
+enum { VC_NORM_NONE = 0, VC_NORM_HEAD = 1, VC_NORM_TOKEN = 2 };
+enum { VC_ROTARY_NONE = 0, VC_ROTARY_INTERLEAVED = 1, VC_ROTARY_HALF = 2 };
+enum { VC_ROPE_SCALING_NONE = 0, VC_ROPE_SCALING_LINEAR = 1, VC_ROPE_SCALING_NTK = 2, VC_ROPE_SCALING_YARN = 3 };
+typedef struct {
+  int32_t B, N, d;                  /* d a multiple of 8, 8 <= d <= 256; 1 <= N <= 2^22; 1 <= B <= 65535   */
+  int32_t H_q, H_k;                 /* 0 <= H <= 65535, not both 0                                         */
+  int32_t dtype, weight_dtype;      /* VC_DTYPE_*                                                          */
+  int32_t norm;                     /* VC_NORM_*                                                           */
+  int32_t rotary;                   /* VC_ROTARY_*                                                         */
+  int32_t rope_dim_t, rope_dim_h, rope_dim_w;   /* even, sum <= d; all 0 => the default of vc_params       */
+  int32_t grid_t, grid_h, grid_w;   /* grid_t * grid_h * grid_w == N unless `positions` is given           */
+  int32_t start_t, start_h, start_w;
+  int32_t rope_scaling;             /* VC_ROPE_SCALING_*                                                   */
+  int32_t rope_original_t, rope_original_h, rope_original_w;
+  float eps;                        /* 0 => 1e-6                                                           */
+  float rope_theta;                 /* 0 => 10000; > 1                                                     */
+  float rope_factor_t, rope_factor_h, rope_factor_w;
+  float yarn_beta_fast, yarn_beta_slow;         /* 0 => 32, 1                                              */
+  float rope_attention_factor;
+  vc_strides q, k, q_out, k_out;
+} vc_qk_params;
+vc_status vc_qk_norm_rope(const vc_qk_params *p, const void *q, const void *k, const void *q_weight,
+                          const void *k_weight, const int32_t *positions, void *q_out, void *k_out, void *stream);
+
+/* A matrix as E4M3 codes with one FP32 scale for each block of 128 columns and block_rows rows (1: activations, 128: weights):
+ *
+ *   a = max(amax of the block, 448 * 2^-100)     scale = a / 448     code = e4m3(x * (448 / a)), to nearest even
+ *
+ * all FP32.  A block that holds an infinity or NaN gets such a scale and stands for NaN throughout.
+ * Row r = b N + n, column c = h d + channel of x [B][H][N][d]: the output of an attention becomes the operand of the
+ * projection behind it without a transposition; a plain matrix is B = H = 1.  The last block of rows or columns may be short.
+ *   codes [B N][H d]     scale [ceil(H d / 128)][B N] (block_rows 1) or [ceil(B N / 128)][ceil(H d / 128)] (128) */
+typedef struct {
+  int32_t B, H, N, d;               /* d a multiple of 8, H * d a multiple of 16, <= 2^20; B * N <= 2^31 - 129 */
+  int32_t dtype;                    /* VC_DTYPE_*                                                          */
+  int32_t block_rows;               /* 1 or 128                                                            */
+  vc_strides x;
+} vc_quant_params;
+vc_status vc_quant_fp8(const vc_quant_params *p, const void *x, void *codes, float *scale, void *stream);
+
 /* Number of kernels this library has launched in this process (diagnostics). */
 uint64_t vc_launch_count(void);
 

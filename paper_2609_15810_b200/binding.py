@@ -62,6 +62,78 @@ class PrepStats(ctypes.Structure):
     _fields_ = [("k_mean", ctypes.c_void_p), ("v_block_mean", ctypes.c_void_p), ("v_amax", ctypes.c_void_p)]
 
 
+VC_DTYPE_BF16, VC_DTYPE_FP16, VC_DTYPE_FP32 = 0, 1, 2
+VC_NORM_NONE, VC_NORM_HEAD, VC_NORM_TOKEN = 0, 1, 2
+VC_ROTARY_NONE, VC_ROTARY_INTERLEAVED, VC_ROTARY_HALF = 0, 1, 2
+VC_ROPE_SCALING_NONE, VC_ROPE_SCALING_LINEAR, VC_ROPE_SCALING_NTK, VC_ROPE_SCALING_YARN = 0, 1, 2, 3
+_DTYPES = {torch.bfloat16: VC_DTYPE_BF16, torch.float16: VC_DTYPE_FP16, torch.float32: VC_DTYPE_FP32}
+
+
+def _dtype(t):
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"element type {t.dtype}: bfloat16, float16 or float32 is wanted")
+    return _DTYPES[t.dtype]
+
+
+class Strides(ctypes.Structure):
+    """Mirror of vc_strides."""
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("n", ctypes.c_int64)]
+
+    @classmethod
+    def of(cls, t):
+        """Of a [B, H, N, d] tensor in elements; its channels have to lie side by side."""
+        if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+            raise ValueError("a [B, H, N, d] tensor with d contiguous is wanted")
+        # strides of dimensions of one entry say nothing; all zero would mean packed
+        n = t.stride(2) if t.shape[2] > 1 else t.shape[3]
+        return cls(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0, n)
+
+
+class QkParams(ctypes.Structure):
+    """Mirror of vc_qk_params."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "N", "d", "H_q", "H_k", "dtype", "weight_dtype", "norm", "rotary",
+                                               "rope_dim_t", "rope_dim_h", "rope_dim_w", "grid_t", "grid_h", "grid_w",
+                                               "start_t", "start_h", "start_w", "rope_scaling",
+                                               "rope_original_t", "rope_original_h", "rope_original_w")] +
+                [(n, ctypes.c_float) for n in ("eps", "rope_theta", "rope_factor_t", "rope_factor_h", "rope_factor_w",
+                                               "yarn_beta_fast", "yarn_beta_slow", "rope_attention_factor")] +
+                [(n, Strides) for n in ("q", "k", "q_out", "k_out")])
+
+    @classmethod
+    def of(cls, q, k, q_out, k_out, grid=(0, 0, 0), weight=None, rope_dims=(0, 0, 0), start=(0, 0, 0), rope_factor=(0.0, 0.0, 0.0),
+           rope_original=(0, 0, 0), **kw):
+        """For [B, H, N, d] tensors, either of q and k (with its output) None; the triples run over (t, h, w)."""
+        x = q if q is not None else k
+        B, _, N, d = x.shape
+        p = cls(B=B, N=N, d=d, dtype=_dtype(x), weight_dtype=_dtype(x if weight is None else weight))
+        for name, t, out in (("q", q, q_out), ("k", k, k_out)):
+            if t is None:
+                continue
+            if t.shape != out.shape or t.shape[0] != B or t.shape[2:] != x.shape[2:] or t.dtype != x.dtype or out.dtype != x.dtype:
+                raise ValueError("q, k and their outputs differ in batches, tokens, head dimension or type")
+            setattr(p, "H_" + name, t.shape[1])
+            setattr(p, name, Strides.of(t))
+            setattr(p, name + "_out", Strides.of(out))
+        for field, values in (("grid", grid), ("rope_dim", rope_dims), ("start", start), ("rope_factor", rope_factor), ("rope_original", rope_original)):
+            for axis, v in zip("thw", values):
+                setattr(p, f"{field}_{axis}", v)
+        for name, v in kw.items():
+            setattr(p, name, v)
+        return p
+
+
+class QuantParams(ctypes.Structure):
+    """Mirror of vc_quant_params."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "N", "d", "dtype", "block_rows")] + [("x", Strides)]
+
+    @classmethod
+    def of(cls, x, block_rows=1):
+        """For a [B, H, N, d] tensor (rows b N + n, columns h d + channel) or a matrix [rows, columns]."""
+        x = x if x.dim() == 4 else x[None, None]
+        B, H, N, d = x.shape
+        return cls(B=B, H=H, N=N, d=d, dtype=_dtype(x), block_rows=block_rows, x=Strides.of(x))
+
+
 _lib = None
 
 
@@ -111,6 +183,10 @@ def load_library():
     lib.vc_mma_peak.restype = ctypes.c_int
     lib.vc_mma_peak.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, ctypes.POINTER(ctypes.c_double),
                                 ctypes.POINTER(ctypes.c_double), vp]
+    lib.vc_qk_norm_rope.restype = ctypes.c_int
+    lib.vc_qk_norm_rope.argtypes = [ctypes.POINTER(QkParams)] + [vp] * 8
+    lib.vc_quant_fp8.restype = ctypes.c_int
+    lib.vc_quant_fp8.argtypes = [ctypes.POINTER(QuantParams)] + [vp] * 4
     lib.vc_launch_count.restype = ctypes.c_uint64
     lib.vc_launch_count.argtypes = []
     lib.vc_status_string.restype = ctypes.c_char_p
@@ -258,6 +334,72 @@ def vc_mma_peak(kind, groups=4096):
     _check(load_library().vc_mma_peak(int(kind), int(groups), _ptr(scratch), ctypes.byref(tf), ctypes.byref(mac), _stream()),
            "vc_mma_peak")
     return tf.value, mac.value
+
+
+_TORCH = (torch.bfloat16, torch.float16, torch.float32)
+_FP32, _INT32, _BYTES, _MASK, _CODES = (torch.float32,), (torch.int32,), (torch.uint8,), (torch.bool, torch.uint8), (torch.float8_e4m3fn, torch.uint8)
+
+
+def _types(code):
+    if not 0 <= code < len(_TORCH):
+        raise ValueError(f"element type {code}: VC_DTYPE_BF16, VC_DTYPE_FP16 or VC_DTYPE_FP32 is wanted")
+    return (_TORCH[code],)
+
+
+def _tensor(name, t, device, dtypes, shape=None, strides=None):
+    """The address of a tensor of the operators around the attention.  These take tensors of several types and layouts, so the
+    binding compares them with what the parameter block says: the C entry sees addresses alone.  `strides` None: contiguous."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, and the current device is cuda:{device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: {t.dtype}, not {' or '.join(str(d) for d in dtypes)}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, not {shape}")
+    if strides is None:
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: has to be contiguous")
+    elif t.stride() != strides and any(n > 1 and i != w for n, i, w in zip(t.shape, t.stride(), strides)):
+        raise ValueError(f"{name}: strides {t.stride()}, not {strides} as in the parameters")
+    return t.data_ptr()
+
+
+def _heads(name, t, device, dtypes, shape, s):
+    """The same for a [B, H, N, d] tensor under the vc_strides of the parameter block."""
+    b, h, n = s.b, s.h, s.n
+    _, H, N, d = shape
+    return _tensor(name, t, device, dtypes, shape, (b, h, n, 1) if b or h or n else (H * N * d, N * d, d, 1))
+
+
+def vc_qk_norm_rope(p, q, k, q_weight, k_weight, positions, q_out, k_out):
+    """RMS norm (p.norm) and rotation (p.rotary) of q and k into q_out and k_out; q, k, a weight or positions may be None."""
+    lib, dev, dt, wt = load_library(), torch.cuda.current_device(), _types(p.dtype), _types(p.weight_dtype)
+    qs, ks = (p.B, p.H_q, p.N, p.d), (p.B, p.H_k, p.N, p.d)
+    heads = p.norm == VC_NORM_TOKEN
+    _check(lib.vc_qk_norm_rope(ctypes.byref(p), _heads("q", q, dev, dt, qs, p.q), _heads("k", k, dev, dt, ks, p.k),
+                               _weight("q_weight", q_weight, dev, wt, p.d * (p.H_q if heads else 1)),
+                               _weight("k_weight", k_weight, dev, wt, p.d * (p.H_k if heads else 1)),
+                               _tensor("positions", positions, dev, _INT32, (p.B, p.N, 3)),
+                               _heads("q_out", q_out, dev, dt, qs, p.q_out), _heads("k_out", k_out, dev, dt, ks, p.k_out), _stream()),
+           "vc_qk_norm_rope")
+
+
+def _weight(name, t, device, dtypes, count):
+    if t is not None and t.numel() != count:
+        raise ValueError(f"{name}: {t.numel()} elements, not {count}")
+    return _tensor(name, t, device, dtypes)
+
+
+def vc_quant_fp8(p, x, codes, scale):
+    """E4M3 codes [B N, H d] (float8_e4m3fn or uint8) and FP32 scales of x, [B, H, N, d] or a matrix [rows, columns]."""
+    lib, dev = load_library(), torch.cuda.current_device()
+    rows, cols = p.B * p.N, p.H * p.d
+    nb = (cols + 127) // 128
+    _check(lib.vc_quant_fp8(ctypes.byref(p), _heads("x", x if x.dim() == 4 else x[None, None], dev, _types(p.dtype), (p.B, p.H, p.N, p.d), p.x),
+                            _tensor("codes", codes, dev, _CODES, (rows, cols)),
+                            _tensor("scale", scale, dev, _FP32, (nb, rows) if p.block_rows == 1 else ((rows + 127) // 128, nb)), _stream()),
+           "vc_quant_fp8")
 
 
 def vc_launch_count():

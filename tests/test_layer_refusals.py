@@ -1,0 +1,92 @@
+"""What the operators around the quantized attention refuse, on the host and before any launch (no GPU)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2609_15810_b200 as vc
+from paper_2609_15810_b200.binding import QkParams, QuantParams, Strides
+
+P = 4096          # stands for an aligned address: a refused call never looks at it
+
+
+def _qk(lib=None, ptrs=(P, P, P, P, P, P, P), **kw):
+    p = QkParams(B=1, N=24, d=64, H_q=2, H_k=2, grid_t=2, grid_h=3, grid_w=4, norm=vc.VC_NORM_HEAD, rotary=vc.VC_ROTARY_HALF)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    q, k, wq, wk, pos, qo, ko = ptrs
+    return vc.load_library().vc_qk_norm_rope(ctypes.byref(p), q, k, wq, wk, pos, qo, ko, None)
+
+
+NO_POS = (P, P, P, P, None, 2 * P, 2 * P)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=0), dict(B=65536), dict(N=0), dict(N=(1 << 22) + 1), dict(d=0), dict(d=60), dict(d=264), dict(H_q=0, H_k=0), dict(H_q=-1), dict(H_k=65536),
+    dict(dtype=3), dict(dtype=-1), dict(weight_dtype=3), dict(norm=3), dict(norm=-1), dict(rotary=3), dict(rotary=-1), dict(eps=-1.0), dict(eps=float("nan")),
+    dict(grid_t=3), dict(grid_h=0), dict(grid_w=-4), dict(start_t=2 ** 31 - 2), dict(rope_dim_t=3, rope_dim_h=5), dict(rope_dim_t=-2, rope_dim_h=4),
+    dict(rope_dim_t=60, rope_dim_h=8), dict(rope_theta=0.5), dict(rope_theta=float("inf")), dict(rope_theta=float("nan")), dict(rope_scaling=4),
+    dict(rope_scaling=-1), dict(rope_factor_t=-1.0), dict(rope_factor_w=float("nan")), dict(rope_attention_factor=-1.0), dict(yarn_beta_fast=-2.0),
+    dict(rope_scaling=vc.VC_ROPE_SCALING_YARN),
+    dict(q=Strides(0, 0, 63)), dict(q=Strides(0, 0, 68)), dict(B=2, k=Strides(-64, 64, 64)), dict(q=Strides(0, 3, 64)), dict(q_out=Strides(0, 0, 64)),
+    dict(q=Strides(0, 1 << 40, 64)), dict(k_out=Strides(1536, 1536, 32))])
+def test_qk_norm_rope_parameters(kw):
+    assert _qk(ptrs=NO_POS, **kw) == vc.VC_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("at", range(7))
+def test_qk_norm_rope_pointers(at):
+    ptrs = [P, 3 * P, P, P, P, 2 * P, 4 * P]
+    ptrs[at] += 8
+    assert _qk(ptrs=ptrs) == vc.VC_ERR_INVALID_ARG
+    if at in (0, 1, 5, 6):
+        ptrs[at] = None
+        assert _qk(ptrs=ptrs) == vc.VC_ERR_INVALID_ARG
+
+
+def test_qk_norm_rope_in_place_wants_the_same_strides():
+    assert _qk(ptrs=(P, P, P, P, None, P, 2 * P), q_out=Strides(0, 64, 128)) == vc.VC_ERR_INVALID_ARG
+
+
+def _quant(x=P, codes=P, scale=P, **kw):
+    p = QuantParams(B=1, H=2, N=5, d=64, block_rows=1)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return vc.load_library().vc_quant_fp8(ctypes.byref(p), x, codes, scale, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=None), dict(codes=None), dict(scale=None), dict(x=P + 8), dict(codes=P + 1), dict(scale=P + 4), dict(B=0), dict(H=0), dict(N=0), dict(d=0),
+    dict(d=12), dict(H=1, d=24), dict(H=1 << 15), dict(B=1 << 16, N=1 << 15), dict(dtype=5), dict(block_rows=0), dict(block_rows=64)])
+def test_quant_fp8(kw):
+    assert _quant(**kw) == vc.VC_ERR_INVALID_ARG
+
+
+def test_no_parameters():
+    lib = vc.load_library()
+    assert lib.vc_qk_norm_rope(None, P, P, P, P, P, P, P, None) == vc.VC_ERR_INVALID_ARG
+    assert lib.vc_quant_fp8(None, P, P, P, None) == vc.VC_ERR_INVALID_ARG
+
+
+def test_parameter_blocks_from_tensors():
+    x = torch.zeros(2, 6, 3, 64, dtype=torch.float16).transpose(1, 2)          # [B, H, N, d] of [B, N, H, d] memory
+    p = QkParams.of(x, None, torch.zeros(2, 3, 6, 64, dtype=torch.float16), None, grid=(1, 2, 3))
+    assert (p.B, p.N, p.d, p.H_q, p.H_k, p.dtype, p.grid_h, p.grid_w) == (2, 6, 64, 3, 0, vc.VC_DTYPE_FP16, 2, 3)
+    assert (p.q.b, p.q.h, p.q.n) == (6 * 3 * 64, 64, 3 * 64) and (p.q_out.b, p.q_out.h, p.q_out.n) == (3 * 6 * 64, 6 * 64, 64)
+    with pytest.raises(ValueError):
+        QkParams.of(x, x[:, :, :5], x, x[:, :, :5])
+    with pytest.raises(ValueError):
+        QkParams.of(x, None, x.float(), None)
+    with pytest.raises(ValueError):
+        QuantParams.of(x.transpose(2, 3))
+    with pytest.raises(ValueError):
+        QuantParams.of(x.to(torch.float64))
+    m = QuantParams.of(torch.zeros(7, 48), 128)
+    assert (m.B, m.H, m.N, m.d, m.block_rows, m.dtype) == (1, 1, 7, 48, 128, vc.VC_DTYPE_FP32)
+
+
+def test_sizes_of_the_parameter_blocks():
+    """The C structs have no padding the mirrors lack: 8-byte members start on 8-byte boundaries."""
+    assert ctypes.sizeof(Strides) == 24
+    assert ctypes.sizeof(QkParams) == 22 * 4 + 8 * 4 + 4 * 24
+    assert ctypes.sizeof(QuantParams) == 6 * 4 + 24
