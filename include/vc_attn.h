@@ -394,6 +394,33 @@ typedef struct {
 vc_status vc_qk_norm_rope(const vc_qk_params *p, const void *q, const void *k, const void *q_weight,
                           const void *k_weight, const int32_t *positions, void *q_out, void *k_out, void *stream);
 
+/* Attention of N_q queries to the N_kv states of an encoder, per (b, h):
+ *
+ *   o = softmax(softmax_scale q k^T over the kept keys) v        lse = ln sum exp(softmax_scale q k^T)
+ *
+ * Key j of batch b is kept if j < kv_len[b] (int32 [B], clamped into [0, N_kv]; NULL = N_kv) and key_mask[b][j] != 0
+ * (bytes [B][N_kv]; NULL = all).  What the others hold is not used, infinities and NaN included.  With no key kept
+ * the row is 0 and its lse -infinity.  H_kv divides H: heads h of Q with the same h / (H / H_kv) share keys and values.
+ * Scores, maxima, sums and the output's accumulators are FP32; probabilities are rounded to the tensors' type in front of
+ * the second product, as its operand.  lse: fp32 [B][H][N_q], or NULL.
+ * Few rows against many keys: the keys of a row are split between CTAs and joined by a second launch, in a
+ * fixed order; key_splits = 1 forbids it, 0 leaves the number to the library.
+ * workspace: vc_cross_workspace_bytes(p) bytes; contents on entry irrelevant, its first 4 bytes become the status word
+ * (vc_poll_status).  Calls that may overlap need workspaces of their own. */
+typedef struct {
+  int32_t B, H, H_kv;               /* B * H <= 65535                                                      */
+  int32_t N_q, N_kv;                /* 1 <= N_q <= 2^22, 0 <= N_kv <= 2^22                                 */
+  int32_t d;                        /* 64 or 128                                                           */
+  int32_t dtype;                    /* VC_DTYPE_BF16 or VC_DTYPE_FP16                                      */
+  int32_t key_splits;               /* 0 <= key_splits <= 64                                               */
+  float softmax_scale;              /* 0 => 1/sqrt(d); > 0                                                 */
+  vc_strides q, k, v, o;
+} vc_cross_params;
+size_t vc_cross_workspace_bytes(const vc_cross_params *p);
+vc_status vc_cross_attn(const vc_cross_params *p, const void *q, const void *k, const void *v,
+                        const int32_t *kv_len, const uint8_t *key_mask, void *o, float *lse,
+                        void *workspace, void *stream);
+
 /* A matrix as E4M3 codes with one FP32 scale for each block of 128 columns and block_rows rows (1: activations, 128: weights):
  *
  *   a = max(amax of the block, 448 * 2^-100)     scale = a / 448     code = e4m3(x * (448 / a)), to nearest even

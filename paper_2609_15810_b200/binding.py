@@ -122,6 +122,23 @@ class QkParams(ctypes.Structure):
         return p
 
 
+class CrossParams(ctypes.Structure):
+    """Mirror of vc_cross_params."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "H", "H_kv", "N_q", "N_kv", "d", "dtype", "key_splits")] +
+                [("softmax_scale", ctypes.c_float)] + [(n, Strides) for n in ("q", "k", "v", "o")])
+
+    @classmethod
+    def of(cls, q, k, v, o, **kw):
+        """For q, o [B, H, N_q, d] and k, v [B, H_kv, N_kv, d]."""
+        B, H, Nq, d = q.shape
+        if k.shape != v.shape or o.shape != q.shape or k.shape[0] != B or k.shape[3] != d or not q.dtype == k.dtype == v.dtype == o.dtype:
+            raise ValueError("q, k, v and o differ in batches, head dimension or type")
+        p = cls(B=B, H=H, H_kv=k.shape[1], N_q=Nq, N_kv=k.shape[2], d=d, dtype=_dtype(q), q=Strides.of(q), k=Strides.of(k), v=Strides.of(v), o=Strides.of(o))
+        for name, val in kw.items():
+            setattr(p, name, val)
+        return p
+
+
 class QuantParams(ctypes.Structure):
     """Mirror of vc_quant_params."""
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "N", "d", "dtype", "block_rows")] + [("x", Strides)]
@@ -185,6 +202,10 @@ def load_library():
                                 ctypes.POINTER(ctypes.c_double), vp]
     lib.vc_qk_norm_rope.restype = ctypes.c_int
     lib.vc_qk_norm_rope.argtypes = [ctypes.POINTER(QkParams)] + [vp] * 8
+    lib.vc_cross_workspace_bytes.restype = ctypes.c_size_t
+    lib.vc_cross_workspace_bytes.argtypes = [ctypes.POINTER(CrossParams)]
+    lib.vc_cross_attn.restype = ctypes.c_int
+    lib.vc_cross_attn.argtypes = [ctypes.POINTER(CrossParams)] + [vp] * 9
     lib.vc_quant_fp8.restype = ctypes.c_int
     lib.vc_quant_fp8.argtypes = [ctypes.POINTER(QuantParams)] + [vp] * 4
     lib.vc_launch_count.restype = ctypes.c_uint64
@@ -389,6 +410,28 @@ def _weight(name, t, device, dtypes, count):
     if t is not None and t.numel() != count:
         raise ValueError(f"{name}: {t.numel()} elements, not {count}")
     return _tensor(name, t, device, dtypes)
+
+
+def vc_cross_workspace_bytes(p):
+    return int(load_library().vc_cross_workspace_bytes(ctypes.byref(p)))
+
+
+def _workspace(t, device, need, where):
+    if need == 0:
+        raise VcError(VC_ERR_INVALID_ARG, where)
+    if t is not None and t.numel() < need:
+        raise ValueError(f"workspace: {t.numel()} bytes, not {need}")
+    return _tensor("workspace", t, device, _BYTES)
+
+
+def vc_cross_attn(p, q, k, v, kv_len, key_mask, o, lse, workspace):
+    """o = softmax(scale q k^T over the kept keys) v; kv_len int32 [B], key_mask bool or uint8 [B, N_kv] and lse fp32 [B, H, N_q] may be None."""
+    lib, dev, dt = load_library(), torch.cuda.current_device(), _types(p.dtype)
+    qs, ks = (p.B, p.H, p.N_q, p.d), (p.B, p.H_kv, p.N_kv, p.d)
+    _check(lib.vc_cross_attn(ctypes.byref(p), _heads("q", q, dev, dt, qs, p.q), _heads("k", k, dev, dt, ks, p.k), _heads("v", v, dev, dt, ks, p.v),
+                             _tensor("kv_len", kv_len, dev, _INT32, (p.B,)), _tensor("key_mask", key_mask, dev, _MASK, (p.B, p.N_kv)),
+                             _heads("o", o, dev, dt, qs, p.o), _tensor("lse", lse, dev, _FP32, (p.B, p.H, p.N_q)),
+                             _workspace(workspace, dev, vc_cross_workspace_bytes(p), "vc_cross_attn"), _stream()), "vc_cross_attn")
 
 
 def vc_quant_fp8(p, x, codes, scale):

@@ -1,0 +1,632 @@
+// vc_cross_attn: attention of queries to an encoder's keys and values, at 16 bits on the tensor cores.
+//
+// A persistent CTA works through items: one or two 128-row query tiles of a head against the head's key tiles (128 keys each), or a
+// part of them.  Warps 0-3 and 4-7 are the softmax of the two query tiles, 8-11 the epilogue, 12 loads, 13 issues the
+// products, 14 clears value rows of masked keys.
+//
+//   S_t = Q_t K^T    both operands in shared memory, K-major, FP32 accumulators in 128 columns of tensor memory
+//   P_t = 2^(s S_t - m)  in registers, a thread per row; written back as 16-bit values over S_t's own columns
+//   O_t += P_t V     P_t from tensor memory, V as it was loaded ([key][channel], read MN-major)
+//
+// The running maximum m of a row is a reference, not the exact maximum: O_t and the row sum are rescaled only when a tile
+// exceeds it by a factor of 2^8 (P_t then holds values up to 2^8, which both types do).  The first tile sets it,
+// so a rescale is rare, and the softmax warps do it themselves: S_t(j) complete says that the product of tile j - 1,
+// issued in front of it, is complete too.
+//
+// Bound by the tensor cores and the special-function unit together: a pair of tiles of 128 keys takes 2048 cycles of either at
+// d = 128 (4 products of 512 cycles; 32768 exponentials, 16 a cycle).
+#include <cmath>
+#include <type_traits>
+
+#include "vc_attn_shared.cuh"
+#include "vc_layer.cuh"
+#include "vc_sm100.cuh"
+
+namespace vc {
+namespace {
+
+using namespace layer;
+using namespace sm100;
+
+constexpr int kThreads = 512, kStages = 4;
+constexpr int kSms = 148;                         // what the rule for splits counts on: the workspace's size must not vary
+constexpr float kRescale = 8.0f;                  // log2 of the factor a row may exceed its reference by
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct CrossArgs {
+  void* o;
+  float *lse, *part_o, *part_lse;                 // part_*: [splits][B * H][N_q] of keys split between CTAs
+  const int32_t* kv_len;
+  const uint8_t* key_mask;
+  uint32_t* status;
+  vc_strides so;
+  int heads, H, group, Nq, Nkv;                   // heads: B * H
+  int qtiles, qitems, tiles_per_item, splits, items;
+  int q_b, q_h, k_b, k_h, v_b, v_h;               // 1, or 0 for a dimension that is broadcast: multiplies the copy's coordinate
+  float sl;                                       // softmax_scale * log2(e)
+  uint32_t limit, nonblocking;
+};
+
+struct Smem {
+  uint64_t full[kStages], empty[kStages], fixed[2];
+  uint64_t q_full[2], q_free[2], s_full[2], p_full[2], o_full[2], o_free[2], drain;
+  alignas(16) uint32_t bits[4][4];                // kept keys of a tile
+  float2 ml[2][2][128];                           // [a tile's items in turn][query tile][row]: reference, row sum
+  uint32_t tmem_base;
+  volatile int abort;
+};
+
+struct Item {
+  int b, h, q0, split, t0, nt, len;
+  bool two;
+};
+
+__device__ __forceinline__ Item item_of(const CrossArgs& a, int idx) {
+  Item w;
+  const int u = idx / a.splits, bh = u / a.qitems;
+  w.split = idx - u * a.splits;
+  w.q0 = (u - bh * a.qitems) * a.tiles_per_item;
+  w.b = bh / a.H;
+  w.h = bh - w.b * a.H;
+  w.two = a.tiles_per_item == 2 && w.q0 + 1 < a.qtiles;
+  w.len = a.kv_len ? min(max(__ldg(a.kv_len + w.b), 0), a.Nkv) : a.Nkv;
+  const int tiles = (w.len + 127) >> 7, per = (tiles + a.splits - 1) / a.splits;
+  w.t0 = w.split * per;
+  w.nt = max(0, min(per, tiles - w.t0));
+  return w;
+}
+
+// Bounded wait of a whole warp (see warp_wait2 of the quantized kernels: a bare test in front, one vote a poll).
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, Smem* sh, const CrossArgs& a, uint32_t code) {
+  if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
+#pragma unroll 1
+  for (uint32_t i = 0; i < a.limit; ++i) {
+    if (__all_sync(0xffffffffu, a.nonblocking ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity))) return true;
+    if ((i & 63u) == 63u && __any_sync(0xffffffffu, sh->abort)) return false;
+  }
+  sh->abort = 1;
+  // CTA 0 clears the word when it starts; a wait that gave up started later and took longer, but for a test's tiny limit
+  __nanosleep(20000);
+  atomicExch(a.status, kStatusTimeout | code);
+  return false;
+}
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+
+// MN-major operand in the 128-byte swizzle: rows of 64 channels of one key, 8 keys a kilobyte, the next 64 channels a panel on.
+__device__ __forceinline__ uint64_t desc_mnmajor(uint32_t saddr, uint32_t panel_bytes) {
+  return (uint64_t)((saddr & 0x3FFFF) >> 4) | (uint64_t)(panel_bytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+template <typename T> __device__ constexpr uint32_t idesc16(int M, int N) {       // T x T -> FP32, both K-major
+  return (1u << 4) | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+constexpr uint32_t kPanel = 128 * 128;            // 128 rows of 64 16-bit channels
+
+template <int D> struct Lay {
+  static constexpr uint32_t kTile = kPanel * (D / 64);         // a query, key or value tile
+  static constexpr uint32_t kOut = kPanel;                     // 64 channels of an output tile
+  static constexpr uint32_t kSmem = 2 * kTile + kStages * kTile + kOut + (uint32_t)sizeof(Smem);
+  // S_t at 128 t (P_t over its first half), O_t behind
+  static constexpr uint32_t kO = 256, kOStride = D;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                  const __grid_constant__ CrossArgs a) {
+  using L = Lay<D>;
+  constexpr int kRegSoftmax = 184, kRegEpi = 104, kRegCtl = 40;
+  static_assert(2 * kRegSoftmax + kRegEpi + kRegCtl <= 4 * 128, "register budget exceeds the CTA's allocation");
+  static_assert(L::kSmem <= 227 * 1024, "shared memory of the kernel exceeds the SM");
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* sQ = smem;
+  unsigned char* sKV = smem + 2 * L::kTile;
+  unsigned char* sOut = sKV + kStages * L::kTile;
+  Smem* sh = reinterpret_cast<Smem*>(sOut + L::kOut);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const bool masked = a.kv_len || a.key_mask;       // some value row may have to be cleared
+
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 1); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&sh->fixed[t], 1);
+      mbar_init(&sh->q_full[t], 1); mbar_init(&sh->q_free[t], 1);
+      mbar_init(&sh->s_full[t], 1); mbar_init(&sh->p_full[t], 128);
+      mbar_init(&sh->o_full[t], 1); mbar_init(&sh->o_free[t], 128);
+    }
+    mbar_init(&sh->drain, 1);
+    sh->abort = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tm_q); tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v);
+  }
+  pdl_wait();
+  if (warp == 14) { tmem_alloc<512>(&sh->tmem_base); tmem_relinquish(); }
+  if (tid == 0 && blockIdx.x == 0) *a.status = 0;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh->tmem_base;
+  const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+
+  if (warp >= 12) {
+    reg_dec<kRegCtl>();
+    if (warp == 12) {
+      // -------------------------------------------------------------------------------- loads
+      int g = 0, n[2] = {0, 0};                     // key tiles; items of each query tile
+      int issued = 0;                               // ring slots filled
+      bool ok = true;
+      auto fill = [&](const CUtensorMap* m, int row, int ch, int cb) {
+        const int st = issued % kStages;
+        if (!(ok = wait(&sh->empty[st], ((issued / kStages) & 1) ^ 1, sh, a, 1))) return;
+        if (elect_one()) {
+          mbar_expect_tx(&sh->full[st], L::kTile);
+          for (int c = 0; c < D / 64; ++c) tma_load_4d(sKV + st * L::kTile + c * kPanel, m, &sh->full[st], 64 * c, row, ch, cb);
+        }
+        __syncwarp();
+        ++issued;
+      };
+      for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+        const Item w = item_of(a, idx);
+        if (w.nt == 0) continue;
+        const int hk = w.h / a.group;
+        for (int j = 0; ok && j < w.nt; ++j, ++g) {
+          const int row = (w.t0 + j) * 128;
+          // the slot's last readers are four key tiles back, and this tile's copy waits for the keys of two tiles back
+          uint32_t words[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = row + 32 * i + lane;
+            bool keep = key < w.len;
+            if (a.key_mask && keep) keep = __ldg(a.key_mask + (int64_t)w.b * a.Nkv + key) != 0;
+            words[i] = __ballot_sync(0xffffffffu, keep);
+          }
+          if (!(ok = wait(&sh->empty[issued % kStages], ((issued / kStages) & 1) ^ 1, sh, a, 2))) break;
+          if (lane < 4) sh->bits[g & 3][lane] = lane == 0 ? words[0] : lane == 1 ? words[1] : lane == 2 ? words[2] : words[3];
+          __syncwarp();
+          fill(&tm_k, row, hk * a.k_h, w.b * a.k_b);
+          if (!ok) break;
+          if (j == 0) {
+            for (int t = 0; ok && t < (w.two ? 2 : 1); ++t, ++n[t - 1]) {
+              if (!(ok = wait(&sh->q_free[t], (n[t] & 1) ^ 1, sh, a, 3))) break;
+              if (elect_one()) {
+                mbar_expect_tx(&sh->q_full[t], L::kTile);
+                for (int c = 0; c < D / 64; ++c)
+                  tma_load_4d(sQ + t * L::kTile + c * kPanel, &tm_q, &sh->q_full[t], 64 * c, (w.q0 + t) * 128, w.h * a.q_h, w.b * a.q_b);
+              }
+              __syncwarp();
+            }
+            if (!ok) break;
+          }
+          fill(&tm_v, row, hk * a.v_h, w.b * a.v_b);
+        }
+      }
+      // every copy issued has landed before the CTA may end (at once on a normal run)
+      for (int t = 0; t < 2; ++t)
+        if (n[t]) mbar_wait(&sh->q_full[t], (n[t] - 1) & 1, attn::kDrainLimit);
+      for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(&sh->full[i % kStages], (i / kStages) & 1, attn::kDrainLimit);
+    } else if (warp == 13) {
+      // -------------------------------------------------------------------------------- products
+      constexpr uint32_t idesc_s = idesc16<T>(128, 128), idesc_o = idesc16<T>(128, D) | (1u << 16);
+      struct Pos { int idx, j, g; Item w; };
+      Pos cur{(int)blockIdx.x - (int)gridDim.x, 0, 0, {}};
+      auto next = [&](Pos& p) {                     // to the next key tile; false behind the last one
+        if (++p.j < p.w.nt) { ++p.g; return true; }
+        do {
+          p.idx += gridDim.x;
+          if (p.idx >= a.items) return false;
+          p.w = item_of(a, p.idx);
+        } while (p.w.nt == 0);
+        p.j = 0;
+        ++p.g;
+        return true;
+      };
+      cur.g = -1;
+      int nq[2] = {0, 0}, no[2] = {0, 0}, np[2] = {0, 0};       // uses of Q_t, O_t, P_t
+      bool ok = true;
+      auto scores = [&](const Pos& p, int t) {
+        const int slot = 2 * p.g, st = slot % kStages;
+        if (t == 0 && !(ok = wait(&sh->full[st], (slot / kStages) & 1, sh, a, 10))) return;
+        if (p.j == 0) {
+          if (!(ok = wait(&sh->q_full[t], nq[t] & 1, sh, a, 11))) return;
+          ++nq[t];
+        }
+        if (elect_one()) {
+          tc_fence_after();
+          const uint64_t dq = smem_desc_kmajor(smem_u32(sQ + t * L::kTile), 128), dk = smem_desc_kmajor(smem_u32(sKV + st * L::kTile), 128);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t at = (k / 4) * (kPanel >> 4) + 2 * (k % 4);
+            mma_f16_ss(tmem + 128 * t, dq + at, dk + at, idesc_s, k > 0);
+          }
+          mma_commit(&sh->s_full[t]);
+          if (p.j == p.w.nt - 1) mma_commit(&sh->q_free[t]);
+          if (t == (p.w.two ? 1 : 0)) mma_commit(&sh->empty[st]);
+        }
+        __syncwarp();
+      };
+      auto outputs = [&](const Pos& p, int t) {
+        const int slot = 2 * p.g + 1, st = slot % kStages;
+        if (t == 0) {
+          if (!(ok = wait(&sh->full[st], (slot / kStages) & 1, sh, a, 12))) return;
+          if (masked && !(ok = wait(&sh->fixed[p.g & 1], (p.g >> 1) & 1, sh, a, 13))) return;
+        }
+        if (p.j == 0) {
+          if (!(ok = wait(&sh->o_free[t], (no[t] & 1) ^ 1, sh, a, 14))) return;
+          ++no[t];
+        }
+        if (!(ok = wait(&sh->p_full[t], np[t] & 1, sh, a, 15))) return;
+        ++np[t];
+        if (elect_one()) {
+          tc_fence_after();
+          const uint64_t dv = desc_mnmajor(smem_u32(sKV + st * L::kTile), kPanel);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) mma_f16_ts(tmem + L::kO + L::kOStride * t, tmem + 128 * t + 8 * k, dv + 128 * k, idesc_o, (p.j > 0) | (k > 0));
+          if (p.j == p.w.nt - 1) mma_commit(&sh->o_full[t]);
+          if (t == (p.w.two ? 1 : 0)) mma_commit(&sh->empty[st]);
+        }
+        __syncwarp();
+      };
+      bool more = next(cur);
+      if (more) {
+        scores(cur, 0);
+        if (ok && cur.w.two) scores(cur, 1);
+      }
+      while (ok && more) {
+        Pos nx = cur;
+        const bool has = next(nx);
+        outputs(cur, 0);
+        if (ok && has) scores(nx, 0);
+        if (ok && cur.w.two) outputs(cur, 1);
+        if (ok && has && nx.w.two) scores(nx, 1);
+        cur = nx;
+        more = has;
+      }
+      if (elect_one()) mma_commit(&sh->drain);
+      __syncwarp();
+      mbar_wait(&sh->drain, 0, attn::kDrainLimit);
+    } else if (warp == 14 && masked) {
+      // -------------------------------------------------------------------------------- value rows of masked keys
+      // 0 times an infinity or NaN is NaN: rows whose probability is 0 must hold numbers.
+      int g = 0;
+      bool ok = true;
+      for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+        const Item w = item_of(a, idx);
+        for (int j = 0; j < w.nt; ++j, ++g) {
+          const int slot = 2 * g + 1, st = slot % kStages;
+          if (!(ok = wait(&sh->full[st], (slot / kStages) & 1, sh, a, 20))) break;
+          const uint4 kept = *reinterpret_cast<const uint4*>(sh->bits[g & 3]);       // (written in front of the keys' copy)
+          if ((kept.x & kept.y & kept.z & kept.w) != 0xffffffffu) {
+            unsigned char* tile = sKV + st * L::kTile;
+#pragma unroll 1
+            for (int r = lane >> 3; r < 128; r += 4) {                               // eight lanes a row
+              const uint32_t word = r < 64 ? (r < 32 ? kept.x : kept.y) : (r < 96 ? kept.z : kept.w);
+              if (!(word >> (r & 31) & 1))
+                for (int c = 0; c < D / 64; ++c) *reinterpret_cast<uint4*>(tile + c * kPanel + r * 128 + 16 * (lane & 7)) = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");             // the stores -> tensor-core reads
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh->fixed[g & 1]);
+          __syncwarp();
+        }
+      }
+    }
+  } else if (warp < 8) {
+    // ---------------------------------------------------------------------------------- softmax, one query tile a warpgroup
+    reg_inc<kRegSoftmax>();
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t s_col = lane_base + 128 * t, o_col = lane_base + L::kO + L::kOStride * t;
+    int g = 0, uses = 0, items = 0;
+    bool ok = true;
+    for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+      const Item w = item_of(a, idx);
+      if (w.nt == 0) continue;
+      if (t && !w.two) { g += w.nt; continue; }
+      float m = -INFINITY, l = 0.f;                 // reference (log2 domain) and row sum
+      for (int j = 0; j < w.nt; ++j, ++g) {
+        if (!(ok = wait(&sh->s_full[t], uses & 1, sh, a, 30))) break;
+        ++uses;
+        tc_fence_after();
+        uint32_t s0[32], s1[32], s2[32], s3[32];
+        tmem_ld32(s_col, s0); tmem_ld32(s_col + 32, s1); tmem_ld32(s_col + 64, s2); tmem_ld32(s_col + 96, s3);
+        tmem_wait_ld();
+        if (w.len - (w.t0 + j) * 128 < 128 || a.key_mask) {
+          const uint4 kept = *reinterpret_cast<const uint4*>(sh->bits[g & 3]);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            if (!(kept.x >> i & 1)) s0[i] = 0xff800000u;
+            if (!(kept.y >> i & 1)) s1[i] = 0xff800000u;
+            if (!(kept.z >> i & 1)) s2[i] = 0xff800000u;
+            if (!(kept.w >> i & 1)) s3[i] = 0xff800000u;
+          }
+        }
+        float mx[4] = {__uint_as_float(s0[0]), __uint_as_float(s1[0]), __uint_as_float(s2[0]), __uint_as_float(s3[0])};
+#pragma unroll
+        for (int i = 1; i < 31; i += 2) {
+          mx[0] = max3(mx[0], __uint_as_float(s0[i]), __uint_as_float(s0[i + 1]));
+          mx[1] = max3(mx[1], __uint_as_float(s1[i]), __uint_as_float(s1[i + 1]));
+          mx[2] = max3(mx[2], __uint_as_float(s2[i]), __uint_as_float(s2[i + 1]));
+          mx[3] = max3(mx[3], __uint_as_float(s3[i]), __uint_as_float(s3[i + 1]));
+        }
+        const float top = a.sl * max3(max3(mx[0], __uint_as_float(s0[31]), mx[1]), max3(__uint_as_float(s1[31]), mx[2], __uint_as_float(s2[31])), fmaxf(mx[3], __uint_as_float(s3[31])));
+        if (j == 0) {
+          m = top;
+        } else if (__any_sync(0xffffffffu, top > m + kRescale)) {
+          const float m_new = fmaxf(m, top), alpha = m == m_new ? 1.f : ex2_approx(m - m_new);
+          l *= alpha;
+          m = m_new;
+          uint32_t r[16];
+#pragma unroll 1
+          for (int c = 0; c < D / 16; ++c) {
+            tmem_ld16(o_col + 16 * c, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+            tmem_st16(o_col + 16 * c, r);
+          }
+        }
+        // (a row without a kept key so far: every score is -infinity, and so is the reference)
+        const float ms = m == -INFINITY ? 0.f : m;
+        const uint64_t sl2 = pack_f32x2(a.sl, a.sl), nm2 = pack_f32x2(-ms, -ms);
+        uint64_t sum0 = 0, sum1 = 0;
+        auto part = [&](const uint32_t (&s)[32], int q) {
+          uint32_t out[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float x0, x1;
+            unpack2(fma2(pack_b32x2(s[2 * i], s[2 * i + 1]), sl2, nm2), x0, x1);
+            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+            const uint64_t pp = pack_f32x2(p0, p1);
+            if (i & 1) sum1 = add2(sum1, pp); else sum0 = add2(sum0, pp);
+            out[i] = pack16<T>(p0, p1);
+          }
+          tmem_st16(s_col + 16 * q, out);
+        };
+        part(s0, 0); part(s1, 1); part(s2, 2); part(s3, 3);
+        float a0, a1;
+        unpack2(add2(sum0, sum1), a0, a1);
+        l += a0 + a1;
+        // In front of the last hand-over: the product behind it, when complete, says that these are there too.  Two slots do: the
+        // tile's next item but one gets here only when the next one's first product has seen the epilogue of this one.
+        if (j == w.nt - 1) sh->ml[items & 1][t][row] = make_float2(m, l);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&sh->p_full[t]);
+      }
+      ++items;
+    }
+  } else {
+    // ---------------------------------------------------------------------------------- epilogue
+    reg_dec<kRegEpi>();
+    using Out = attn::OutTile<64>;                  // rows leave in lines of 128 bytes
+    const int quarter = warp & 3;
+    const uint32_t tile = smem_u32(sOut) + quarter * 32 * Out::ROW;
+    int uses[2] = {0, 0};
+    bool ok = true;
+    for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+      const Item w = item_of(a, idx);
+#pragma unroll 1
+      for (int t = 0; t < (w.two ? 2 : 1); ++t) {
+        const int row0 = (w.q0 + t) * 128 + quarter * 32, rows = min(32, a.Nq - row0);
+        float inv = 0.f, lse2 = -INFINITY;
+        uint32_t out[D / 2];
+        // my row of the outputs' [B * H][N_q], behind those of the splits in front of this one
+        const int64_t line = ((int64_t)w.split * a.heads + w.b * a.H + w.h) * a.Nq + row0 + lane;
+        float* po = a.part_o + line * D;
+        if (w.nt > 0) {
+          if (!(ok = wait(&sh->o_full[t], uses[t] & 1, sh, a, 40))) break;
+          const float2 ml = sh->ml[uses[t] & 1][t][quarter * 32 + lane];
+          ++uses[t];
+          inv = ml.y > 0.f || ml.y != ml.y ? 1.0f / ml.y : 0.f;       // (a sum of NaN makes a row of NaN)
+          lse2 = ml.y == 0.f ? -INFINITY : ml.x + log2f(ml.y);
+          tc_fence_after();
+          const uint32_t o_col = lane_base + L::kO + L::kOStride * t;
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t r[32];
+            tmem_ld32(o_col + 32 * c, r);
+            tmem_wait_ld();
+            if (a.splits > 1) {
+              if (lane < rows)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  reinterpret_cast<float4*>(po)[8 * c + i] = make_float4(__uint_as_float(r[4 * i]) * inv, __uint_as_float(r[4 * i + 1]) * inv,
+                                                                         __uint_as_float(r[4 * i + 2]) * inv, __uint_as_float(r[4 * i + 3]) * inv);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) out[16 * c + i] = pack16<T>(__uint_as_float(r[2 * i]) * inv, __uint_as_float(r[2 * i + 1]) * inv);
+            }
+          }
+          tc_fence_before();
+          mbar_arrive(&sh->o_free[t]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < D / 2; ++i) out[i] = 0;
+          if (a.splits > 1 && lane < rows)
+#pragma unroll 1
+            for (int i = 0; i < D / 4; ++i) reinterpret_cast<float4*>(po)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        if (a.splits > 1) {
+          if (lane < rows) a.part_lse[line] = lse2;
+          continue;
+        }
+        if (a.lse && lane < rows) a.lse[line] = lse2 * kLn2;
+        T* dst = static_cast<T*>(a.o) + w.b * a.so.b + w.h * a.so.h + (int64_t)row0 * a.so.n;
+#pragma unroll
+        for (int half = 0; half < D / 64; ++half) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) sts128(Out::chunk(tile, lane, c), out[32 * half + 4 * c], out[32 * half + 4 * c + 1], out[32 * half + 4 * c + 2], out[32 * half + 4 * c + 3]);
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int r = 4 * k + (lane >> 3), c = lane & 7;
+            if (r < rows) *reinterpret_cast<float4*>(dst + r * a.so.n + 64 * half + 8 * c) = lds128(Out::chunk(tile, r, c));
+          }
+          __syncwarp();
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 14) tmem_dealloc<512>(tmem);
+}
+
+// Joins the parts of a row: o = sum w_s o_s / sum w_s, w_s = 2^(lse_s - max lse), in the order of the splits.  A warp a row.
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+cross_join_kernel(const __grid_constant__ CrossArgs a, int64_t rows) {
+  constexpr int kPer = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  pdl_wait();
+  if (r >= rows) return;
+  float top = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) {
+    const float v = a.part_lse[s * rows + r];
+    top = v != v ? v : fmaxf(top, v);
+    if (v != v) break;
+  }
+  const float base = top == -INFINITY ? 0.f : top;
+  float acc[kPer] = {}, sum = 0.f;
+  for (int s = 0; s < a.splits; ++s) {
+    const float wt = exp2f(a.part_lse[s * rows + r] - base);
+    sum += wt;
+    const float* po = a.part_o + (s * rows + r) * D + lane * kPer;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) acc[i] = fmaf(wt, po[i], acc[i]);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  const int64_t bh = r / a.Nq, n = r - bh * a.Nq, b = bh / a.H, h = bh - b * a.H;
+  T* dst = static_cast<T*>(a.o) + b * a.so.b + h * a.so.h + n * a.so.n + lane * kPer;
+#pragma unroll
+  for (int i = 0; i < kPer; i += 2) reinterpret_cast<uint32_t*>(dst)[i / 2] = pack16<T>(acc[i] * inv, acc[i + 1] * inv);
+  if (a.lse && lane == 0) a.lse[r] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * kLn2;
+}
+
+struct Plan {
+  int qtiles, tiles_per_item, qitems, splits;
+  int64_t rows, items;
+  size_t part_o, part_lse, total;
+};
+
+vc_status resolve(const vc_cross_params* p, vc_cross_params* out, Plan* plan) {
+  if (!p) return VC_ERR_INVALID_ARG;
+  vc_cross_params r = *p;
+  if (r.B < 1 || r.H < 1 || r.H_kv < 1 || r.H % r.H_kv || (int64_t)r.B * r.H > 65535) return VC_ERR_INVALID_ARG;
+  if (r.N_q < 1 || r.N_q > (1 << 22) || r.N_kv < 0 || r.N_kv > (1 << 22)) return VC_ERR_INVALID_ARG;
+  if (r.d != 64 && r.d != 128) return VC_ERR_INVALID_ARG;
+  if (r.dtype != VC_DTYPE_BF16 && r.dtype != VC_DTYPE_FP16) return VC_ERR_INVALID_ARG;
+  if (r.key_splits < 0 || r.key_splits > 64) return VC_ERR_INVALID_ARG;
+  if (r.softmax_scale == 0.f) r.softmax_scale = 1.0f / std::sqrt((float)r.d);
+  if (!(r.softmax_scale > 0.f) || !std::isfinite(r.softmax_scale)) return VC_ERR_INVALID_ARG;
+  const int nk = r.N_kv > 0 ? r.N_kv : 1;
+  if (!resolve_strides(p->q, r.B, r.H, r.N_q, r.d, 2, false, &r.q) || !resolve_strides(p->k, r.B, r.H_kv, nk, r.d, 2, false, &r.k) ||
+      !resolve_strides(p->v, r.B, r.H_kv, nk, r.d, 2, false, &r.v) || !resolve_strides(p->o, r.B, r.H, r.N_q, r.d, 2, true, &r.o))
+    return VC_ERR_INVALID_ARG;
+  Plan pl{};
+  pl.rows = (int64_t)r.B * r.H * r.N_q;
+  pl.qtiles = (r.N_q + 127) / 128;
+  const int64_t bh = (int64_t)r.B * r.H;
+  // Two query tiles an item share the keys' copies; with fewer pairs than SMs the tiles go to CTAs of their own.
+  pl.tiles_per_item = bh * ((pl.qtiles + 1) / 2) >= kSms ? 2 : 1;
+  pl.qitems = (pl.qtiles + pl.tiles_per_item - 1) / pl.tiles_per_item;
+  const int ktiles = (r.N_kv + 127) / 128;
+  pl.splits = r.key_splits;
+  if (pl.splits == 0) {
+    const int64_t room = kSms / (bh * pl.qitems);
+    pl.splits = 1;
+    if (room > 1 && ktiles >= 8) pl.splits = (int)(room < ktiles / 4 ? room : ktiles / 4);
+  }
+  if (pl.splits > ktiles) pl.splits = ktiles > 0 ? ktiles : 1;
+  if (pl.splits > 64) pl.splits = 64;
+  pl.items = bh * pl.qitems * pl.splits;
+  if (pl.items > INT32_MAX) return VC_ERR_UNSUPPORTED;
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  pl.part_o = 256;
+  pl.part_lse = pl.part_o + (pl.splits > 1 ? up((size_t)pl.splits * pl.rows * r.d * 4) : 0);
+  pl.total = pl.part_lse + (pl.splits > 1 ? up((size_t)pl.splits * pl.rows * 4) : 0);
+  *out = r;
+  *plan = pl;
+  return VC_OK;
+}
+
+// [B][H][N][d] of 16-bit elements, boxes of 64 channels x 128 rows in the 128-byte swizzle.  A broadcast dimension becomes one
+// entry (its coordinate is multiplied by 0).
+bool make_map16(CUtensorMap* m, const void* base, const vc_strides& s, int B, int H, int N, int d, int* mul_b, int* mul_h) {
+  attn::EncodeTiledFn fn = attn::encode_fn();
+  if (!fn) return false;
+  *mul_b = s.b != 0; *mul_h = s.h != 0;
+  const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)N, (cuuint64_t)(s.h ? H : 1), (cuuint64_t)(s.b ? B : 1)};
+  const cuuint64_t strides[3] = {(cuuint64_t)s.n * 2, (cuuint64_t)(s.h ? s.h : s.n) * 2, (cuuint64_t)(s.b ? s.b : s.n) * 2};
+  const cuuint32_t box[4] = {64, 128, 1, 1}, step[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int D>
+cudaError_t launch_cross(const vc_cross_params& r, const Plan& pl, CrossArgs& a, const void* q, const void* k, const void* v, cudaStream_t s) {
+  alignas(64) CUtensorMap tq, tk, tv;
+  const bool any = r.N_kv > 0;                      // without keys nothing is loaded, and any valid map will do
+  if (!make_map16(&tq, q, r.q, r.B, r.H, r.N_q, D, &a.q_b, &a.q_h)) return cudaErrorUnknown;
+  tk = tv = tq;
+  if (any && (!make_map16(&tk, k, r.k, r.B, r.H_kv, r.N_kv, D, &a.k_b, &a.k_h) || !make_map16(&tv, v, r.v, r.B, r.H_kv, r.N_kv, D, &a.v_b, &a.v_h)))
+    return cudaErrorUnknown;
+  cudaError_t e = allow_smem<cross_attn_kernel<T, D>>();
+  if (e != cudaSuccess) return e;
+  const int grid = pl.items < sm_count() ? (int)pl.items : sm_count();
+  e = launch_overlapped(cross_attn_kernel<T, D>, dim3((unsigned)grid), kThreads, Lay<D>::kSmem, s, tq, tk, tv, a);
+  if (e != cudaSuccess) return e;
+  count_launches(1);
+  if (pl.splits > 1) {
+    e = launch_overlapped(cross_join_kernel<T, D>, dim3((unsigned)((pl.rows + 7) / 8)), 256, 0, s, a, pl.rows);
+    if (e != cudaSuccess) return e;
+    count_launches(1);
+  }
+  return cudaSuccess;
+}
+
+}  // namespace
+}  // namespace vc
+
+using namespace vc;
+
+extern "C" size_t vc_cross_workspace_bytes(const vc_cross_params* p) {
+  vc_cross_params r;
+  Plan pl;
+  return resolve(p, &r, &pl) == VC_OK ? pl.total : 0;
+}
+
+extern "C" vc_status vc_cross_attn(const vc_cross_params* p, const void* q, const void* k, const void* v, const int32_t* kv_len,
+                                   const uint8_t* key_mask, void* o, float* lse, void* workspace, void* stream) {
+  vc_cross_params r;
+  Plan pl;
+  const vc_status st = resolve(p, &r, &pl);
+  if (st != VC_OK) return st;
+  if (!q || !o || !workspace || (r.N_kv > 0 && (!k || !v))) return VC_ERR_INVALID_ARG;
+  if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(o) || misaligned16(workspace) || ((uintptr_t)kv_len & 3) ||
+      ((uintptr_t)lse & 3))
+    return VC_ERR_INVALID_ARG;
+  CrossArgs a{};
+  a.o = o; a.lse = lse; a.kv_len = kv_len; a.key_mask = key_mask;
+  a.status = (uint32_t*)workspace;
+  a.part_o = (float*)((uint8_t*)workspace + pl.part_o);
+  a.part_lse = (float*)((uint8_t*)workspace + pl.part_lse);
+  a.so = r.o;
+  a.heads = r.B * r.H; a.H = r.H; a.group = r.H / r.H_kv; a.Nq = r.N_q; a.Nkv = r.N_kv;
+  a.qtiles = pl.qtiles; a.qitems = pl.qitems; a.tiles_per_item = pl.tiles_per_item; a.splits = pl.splits; a.items = (int)pl.items;
+  a.sl = r.softmax_scale * kLog2e;
+  a.limit = attn::attn_wait_limit();
+  a.nonblocking = attn::attn_wait_nonblocking();
+  cudaStream_t s = (cudaStream_t)stream;
+  cudaError_t e;
+  if (r.dtype == VC_DTYPE_BF16) e = r.d == 128 ? launch_cross<__nv_bfloat16, 128>(r, pl, a, q, k, v, s) : launch_cross<__nv_bfloat16, 64>(r, pl, a, q, k, v, s);
+  else e = r.d == 128 ? launch_cross<__half, 128>(r, pl, a, q, k, v, s) : launch_cross<__half, 64>(r, pl, a, q, k, v, s);
+  return e == cudaSuccess ? VC_OK : VC_ERR_CUDA;
+}

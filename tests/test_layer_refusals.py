@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2609_15810_b200 as vc
-from paper_2609_15810_b200.binding import QkParams, QuantParams, Strides
+from paper_2609_15810_b200.binding import CrossParams, QkParams, QuantParams, Strides
 
 P = 4096          # stands for an aligned address: a refused call never looks at it
 
@@ -62,8 +62,48 @@ def test_quant_fp8(kw):
     assert _quant(**kw) == vc.VC_ERR_INVALID_ARG
 
 
+def _cross(q=P, k=P, v=P, kv_len=P, mask=P, o=P, lse=P, work=P, **kw):
+    p = CrossParams(B=2, H=4, H_kv=2, N_q=5, N_kv=7, d=64)
+    for n, val in kw.items():
+        setattr(p, n, val)
+    return vc.load_library().vc_cross_attn(ctypes.byref(p), q, k, v, kv_len, mask, o, lse, work, None), vc.vc_cross_workspace_bytes(p)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=0), dict(H=0), dict(H_kv=0), dict(H_kv=3), dict(H_kv=8), dict(B=8192, H=8), dict(N_q=0), dict(N_q=(1 << 22) + 1), dict(N_kv=-1),
+    dict(N_kv=(1 << 22) + 1), dict(d=32), dict(d=96), dict(d=256), dict(dtype=vc.VC_DTYPE_FP32), dict(dtype=-1), dict(key_splits=-1), dict(key_splits=65),
+    dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict({"q": Strides(20 * 64, 5 * 64, 60)}),
+    dict({"k": Strides(1, 7 * 64, 64)}), dict({"v": Strides(14 * 64, -64, 64)}), dict({"o": Strides(0, 5 * 64, 64)}), dict({"o": Strides(20 * 64, 0, 64)})])
+def test_cross_attn_parameters(kw):
+    p = CrossParams(B=2, H=4, H_kv=2, N_q=5, N_kv=7, d=64)
+    for n, val in kw.items():
+        setattr(p, n, val)
+    assert vc.load_library().vc_cross_attn(ctypes.byref(p), P, P, P, P, P, P, P, P, None) == vc.VC_ERR_INVALID_ARG
+    assert vc.vc_cross_workspace_bytes(p) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(work=None), dict(q=P + 8), dict(k=P + 2), dict(v=P + 8),
+                                dict(o=P + 8), dict(work=P + 4), dict(lse=P + 2), dict(kv_len=P + 1)])
+def test_cross_attn_pointers(kw):
+    assert _cross(**kw)[0] == vc.VC_ERR_INVALID_ARG
+
+
+def test_cross_attn_workspace():
+    size = lambda **kw: _size(CrossParams(B=1, H=2, H_kv=2, N_q=1, N_kv=4096, d=128), **kw)
+    def _size(p, **kw):
+        for n, val in kw.items():
+            setattr(p, n, val)
+        return vc.vc_cross_workspace_bytes(p)
+    assert size(key_splits=1) == 256
+    assert size(key_splits=4) >= 256 + 4 * 2 * (128 + 1) * 4
+    assert size(key_splits=64) == size(key_splits=32)            # no more than there are key tiles
+    assert size(N_kv=0) == size(N_kv=128) == 256
+    assert size() >= 256 and size(N_q=100000) == 256             # enough rows: nothing to split
+
+
 def test_no_parameters():
     lib = vc.load_library()
+    assert lib.vc_cross_attn(None, P, P, P, P, P, P, P, P, None) == vc.VC_ERR_INVALID_ARG and lib.vc_cross_workspace_bytes(None) == 0
     assert lib.vc_qk_norm_rope(None, P, P, P, P, P, P, P, None) == vc.VC_ERR_INVALID_ARG
     assert lib.vc_quant_fp8(None, P, P, P, None) == vc.VC_ERR_INVALID_ARG
 
@@ -89,4 +129,5 @@ def test_sizes_of_the_parameter_blocks():
     """The C structs have no padding the mirrors lack: 8-byte members start on 8-byte boundaries."""
     assert ctypes.sizeof(Strides) == 24
     assert ctypes.sizeof(QkParams) == 22 * 4 + 8 * 4 + 4 * 24
+    assert ctypes.sizeof(CrossParams) == 8 * 4 + 4 + 4 + 4 * 24          # 4 bytes of padding in front of the strides, as in C
     assert ctypes.sizeof(QuantParams) == 6 * 4 + 24
