@@ -437,6 +437,24 @@ typedef struct {
 } vc_quant_params;
 vc_status vc_quant_fp8(const vc_quant_params *p, const void *x, void *codes, float *scale, void *stream);
 
+/* Product of two such matrices, y = x w^T + bias (a linear layer with weights [N][K]):
+ *
+ *   y[m][n] = sum over blocks kb of x_scale[kb][m] w_scale[n / 128][kb] (sum of x[m][k] w[n][k] over k in block kb) + bias[n]
+ *
+ * Products are exact, sums FP32, one rounding to out_dtype.  x_codes [M][K] with block_rows = 1, w_codes [N][K] with
+ * block_rows = 128, rows ldx / ldw bytes apart (multiples of 16; 0 = K); out [M][N], rows ldo elements apart (0 = N); bias [N]
+ * or NULL.  Few rows: the sum over K is split between CTAs and joined in a fixed order (k_splits = 1 forbids it,
+ * 0 leaves the number to the library).  workspace: as for vc_cross_attn, vc_linear_workspace_bytes(p) bytes. */
+typedef struct {
+  int32_t M, N, K;                  /* >= 1, M and N <= 2^30, K a multiple of 16, <= 2^20                  */
+  int32_t out_dtype, bias_dtype;    /* VC_DTYPE_*                                                          */
+  int32_t k_splits;                 /* 0 <= k_splits <= 64                                                 */
+  int64_t ldx, ldw, ldo;
+} vc_linear_params;
+size_t vc_linear_workspace_bytes(const vc_linear_params *p);
+vc_status vc_linear_fp8(const vc_linear_params *p, const void *x_codes, const float *x_scale, const void *w_codes,
+                        const float *w_scale, const void *bias, void *out, void *workspace, void *stream);
+
 /* Number of kernels this library has launched in this process (diagnostics). */
 uint64_t vc_launch_count(void);
 

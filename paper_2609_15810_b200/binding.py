@@ -151,6 +151,24 @@ class QuantParams(ctypes.Structure):
         return cls(B=B, H=H, N=N, d=d, dtype=_dtype(x), block_rows=block_rows, x=Strides.of(x))
 
 
+class LinearParams(ctypes.Structure):
+    """Mirror of vc_linear_params."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("M", "N", "K", "out_dtype", "bias_dtype", "k_splits")] +
+                [(n, ctypes.c_int64) for n in ("ldx", "ldw", "ldo")])
+
+    @classmethod
+    def of(cls, x_codes, w_codes, out, bias=None, **kw):
+        """For x_codes [M, K], w_codes [N, K], out [M, N], rows contiguous."""
+        (M, K), (N, K_w) = x_codes.shape, w_codes.shape
+        if K != K_w or out.shape != (M, N) or any(t.stride(1) != 1 and t.shape[1] > 1 for t in (x_codes, w_codes, out)):
+            raise ValueError("x [M, K], w [N, K] and out [M, N] with contiguous rows are wanted")
+        ld = [t.stride(0) if t.shape[0] > 1 else 0 for t in (x_codes, w_codes, out)]
+        p = cls(M=M, N=N, K=K, out_dtype=_dtype(out), bias_dtype=_dtype(out if bias is None else bias), ldx=ld[0], ldw=ld[1], ldo=ld[2])
+        for name, val in kw.items():
+            setattr(p, name, val)
+        return p
+
+
 _lib = None
 
 
@@ -208,6 +226,10 @@ def load_library():
     lib.vc_cross_attn.argtypes = [ctypes.POINTER(CrossParams)] + [vp] * 9
     lib.vc_quant_fp8.restype = ctypes.c_int
     lib.vc_quant_fp8.argtypes = [ctypes.POINTER(QuantParams)] + [vp] * 4
+    lib.vc_linear_workspace_bytes.restype = ctypes.c_size_t
+    lib.vc_linear_workspace_bytes.argtypes = [ctypes.POINTER(LinearParams)]
+    lib.vc_linear_fp8.restype = ctypes.c_int
+    lib.vc_linear_fp8.argtypes = [ctypes.POINTER(LinearParams)] + [vp] * 8
     lib.vc_launch_count.restype = ctypes.c_uint64
     lib.vc_launch_count.argtypes = []
     lib.vc_status_string.restype = ctypes.c_char_p
@@ -443,6 +465,23 @@ def vc_quant_fp8(p, x, codes, scale):
                             _tensor("codes", codes, dev, _CODES, (rows, cols)),
                             _tensor("scale", scale, dev, _FP32, (nb, rows) if p.block_rows == 1 else ((rows + 127) // 128, nb)), _stream()),
            "vc_quant_fp8")
+
+
+def vc_linear_workspace_bytes(p):
+    return int(load_library().vc_linear_workspace_bytes(ctypes.byref(p)))
+
+
+def vc_linear_fp8(p, x_codes, x_scale, w_codes, w_scale, bias, out, workspace):
+    """out = x w^T + bias from codes and scales as vc_quant_fp8 writes them (x with block_rows 1, w with 128); bias [N] or None."""
+    lib, dev = load_library(), torch.cuda.current_device()
+    nb = (p.K + 127) // 128
+    _check(lib.vc_linear_fp8(ctypes.byref(p), _tensor("x_codes", x_codes, dev, _CODES, (p.M, p.K), (p.ldx or p.K, 1)),
+                             _tensor("x_scale", x_scale, dev, _FP32, (nb, p.M)),
+                             _tensor("w_codes", w_codes, dev, _CODES, (p.N, p.K), (p.ldw or p.K, 1)),
+                             _tensor("w_scale", w_scale, dev, _FP32, ((p.N + 127) // 128, nb)),
+                             _tensor("bias", bias, dev, _types(p.bias_dtype), (p.N,)),
+                             _tensor("out", out, dev, _types(p.out_dtype), (p.M, p.N), (p.ldo or p.N, 1)),
+                             _workspace(workspace, dev, vc_linear_workspace_bytes(p), "vc_linear_fp8"), _stream()), "vc_linear_fp8")
 
 
 def vc_launch_count():

@@ -1,0 +1,454 @@
+// vc_linear_fp8: product of two E4M3 matrices with an FP32 scale per block of 128, on the tensor cores.
+//
+//   y[m][n] = sum_kb xs[kb][m] ws[n / 128][kb] S_kb[m][n] + bias[n],   S_kb = the product over the block's 128 columns
+//
+// The scales are arbitrary FP32 numbers and differ from block to block of the common width, so no accumulator can run over
+// blocks: each S_kb is a product of its own (4 instructions of 32 columns into a tensor-memory buffer) and two
+// warpgroups add it, scaled, to sums in registers, 128 columns of a row a thread at most.  Per block and 128 x 256 tile
+// the products take 512 cycles, reading the buffer 256 (512 bytes a cycle) and the additions 256 of the FMA pipe, all three
+// side by side.
+//
+// Rows to A, weights to B (128 x 256 or 128 x 128), or the other way round where there are few rows: then 128 weight
+// rows are A, 16 or 64 rows of x are B, and the launch is bound by reading the weights.  With fewer tiles than SMs the blocks of K are
+// split between CTAs and the parts joined by a second launch in a fixed order.
+#include "vc_attn_shared.cuh"
+#include "vc_layer.cuh"
+#include "vc_sm100.cuh"
+
+namespace vc {
+namespace {
+
+using namespace layer;
+using namespace sm100;
+
+constexpr int kThreads = 384;
+constexpr int kSms = 148;                    // what the rule for splits counts on: the workspace's size must not vary
+
+struct LinearArgs {
+  const float *xs, *ws;
+  const void* bias;
+  void* out;
+  float* part;                               // [splits][M][ldp]
+  uint32_t* status;
+  int64_t ldo, ldp;
+  int M, N, blocks, tiles_b, splits, items;  // blocks: of 128 columns of K; tiles_b: tiles along B
+  int out_dtype, bias_dtype;
+  bool vec;                                  // rows of out start on 16-byte boundaries
+  uint32_t limit, nonblocking;
+};
+
+// SWAP: A = weights (128 rows), B = TN rows of x.  Else A = 128 rows of x, B = TN weights.
+template <bool SWAP, int TN> struct Cfg {
+  static constexpr int kGroups = TN >= 128 ? 2 : 1;            // warpgroups that add
+  static constexpr int kCols = TN / kGroups;                   // columns of a thread
+  static constexpr int kBufs = TN == 256 ? 2 : 4;
+  static constexpr int kTmem = kBufs * TN;                     // 512, 512, 256, 64
+  static constexpr uint32_t kA = 128 * 128, kB = TN * 128, kStage = kA + kB;
+  static constexpr int kStages = TN == 256 ? 4 : TN == 128 ? 6 : 8;
+  static constexpr uint32_t kOut = SWAP ? 0 : 8 * 32 * 128;    // 128 bytes of each warp's 32 rows
+};
+
+template <int STAGES, int BUFS> struct Smem {
+  uint64_t full[STAGES], empty[STAGES], acc_full[BUFS], acc_free[BUFS], drain;
+  uint32_t tmem_base;
+  volatile int abort;
+};
+
+template <class S>
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, S* sh, const LinearArgs& a, uint32_t code) {
+  if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
+#pragma unroll 1
+  for (uint32_t i = 0; i < a.limit; ++i) {
+    if (__all_sync(0xffffffffu, a.nonblocking ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity))) return true;
+    if ((i & 63u) == 63u && __any_sync(0xffffffffu, sh->abort)) return false;
+  }
+  sh->abort = 1;
+  __nanosleep(20000);                        // (CTA 0 clears the word when it starts)
+  atomicExch(a.status, kStatusTimeout | code);
+  return false;
+}
+
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+               "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
+               : "memory");
+}
+
+struct Item { int a0, b0, split, kb0, kb1; };                  // first rows of the tile in A and B; blocks of K
+template <int TN> __device__ __forceinline__ Item item_of(const LinearArgs& a, int idx) {
+  Item w;
+  const int tile = idx / a.splits, ta = tile / a.tiles_b;
+  w.split = idx - tile * a.splits;
+  w.a0 = ta * 128;
+  w.b0 = (tile - ta * a.tiles_b) * TN;
+  w.kb0 = (int)((int64_t)a.blocks * w.split / a.splits);
+  w.kb1 = (int)((int64_t)a.blocks * (w.split + 1) / a.splits);
+  return w;
+}
+
+// The warp's 32 rows of `COLS` FP32 sums -> rows of O in memory, 128 bytes of each at a time through shared memory.
+template <typename O> __device__ __forceinline__ uint4 pack_chunk(const float* f);
+template <> __device__ __forceinline__ uint4 pack_chunk<float>(const float* f) {
+  return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+template <> __device__ __forceinline__ uint4 pack_chunk<__nv_bfloat16>(const float* f) {
+  return make_uint4(pack16<__nv_bfloat16>(f[0], f[1]), pack16<__nv_bfloat16>(f[2], f[3]), pack16<__nv_bfloat16>(f[4], f[5]), pack16<__nv_bfloat16>(f[6], f[7]));
+}
+template <> __device__ __forceinline__ uint4 pack_chunk<__half>(const float* f) {
+  return make_uint4(pack16<__half>(f[0], f[1]), pack16<__half>(f[2], f[3]), pack16<__half>(f[4], f[5]), pack16<__half>(f[6], f[7]));
+}
+template <typename O, int COLS>
+__device__ __forceinline__ void emit_rows(const float (&y)[COLS], uint32_t tile, O* dst, int64_t ld, int rows, int cols, bool vec, int lane) {
+  using Out = attn::OutTile<64>;                               // (128 bytes a row, whatever the type)
+  constexpr int kPer = 16 / sizeof(O), kPass = 8 * kPer;       // elements of 16 and of 128 bytes
+#pragma unroll
+  for (int p = 0; p < COLS / kPass; ++p) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint4 v = pack_chunk<O>(y + p * kPass + c * kPer);
+      sts128(Out::chunk(tile, lane, c), v.x, v.y, v.z, v.w);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int r = 4 * k + (lane >> 3), c = lane & 7, col = p * kPass + c * kPer;
+      if (r < rows && col < cols) {
+        const float4 v = lds128(Out::chunk(tile, r, c));
+        O* at = dst + r * ld + col;
+        if (vec && col + kPer <= cols) {
+          *reinterpret_cast<float4*>(at) = v;
+        } else {
+          const O* e = reinterpret_cast<const O*>(&v);
+#pragma unroll
+          for (int i = 0; i < kPer; ++i)
+            if (col + i < cols) at[i] = e[i];
+        }
+      }
+    }
+    __syncwarp();
+  }
+}
+
+template <bool SWAP, int TN>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ LinearArgs a) {
+  using C = Cfg<SWAP, TN>;
+  using S = Smem<C::kStages, C::kBufs>;
+  constexpr int kRegAdd = 216, kRegCtl = 72;
+  static_assert(2 * kRegAdd + kRegCtl <= 3 * 168, "register budget exceeds the CTA's allocation");
+  static_assert(C::kStages * C::kStage + C::kOut + sizeof(S) <= 227 * 1024, "shared memory of the kernel exceeds the SM");
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* sOut = smem + C::kStages * C::kStage;
+  S* sh = reinterpret_cast<S*>(sOut + C::kOut);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 1); }
+    for (int i = 0; i < C::kBufs; ++i) { mbar_init(&sh->acc_full[i], 1); mbar_init(&sh->acc_free[i], 128 * C::kGroups); }
+    mbar_init(&sh->drain, 1);
+    sh->abort = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tm_a); tma_prefetch_desc(&tm_b);
+  }
+  pdl_wait();
+  if (warp == 10) { tmem_alloc<C::kTmem>(&sh->tmem_base); tmem_relinquish(); }
+  if (tid == 0 && blockIdx.x == 0) *a.status = 0;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh->tmem_base;
+
+  if (warp >= 8) {
+    reg_dec<kRegCtl>();
+    if (warp == 8) {
+      // -------------------------------------------------------------------------------- loads
+      int n = 0;
+      bool ok = true;
+      for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+        const Item w = item_of<TN>(a, idx);
+        for (int kb = w.kb0; kb < w.kb1; ++kb, ++n) {
+          const int st = n % C::kStages;
+          if (!(ok = wait(&sh->empty[st], ((n / C::kStages) & 1) ^ 1, sh, a, 1))) break;
+          if (elect_one()) {
+            unsigned char* base = smem + st * C::kStage;
+            mbar_expect_tx(&sh->full[st], C::kStage);
+            tma_load_2d(base, &tm_a, &sh->full[st], kb * 128, w.a0);
+            tma_load_2d(base + C::kA, &tm_b, &sh->full[st], kb * 128, w.b0);
+          }
+          __syncwarp();
+        }
+      }
+      // every copy issued has landed before the CTA may end (at once on a normal run)
+      for (int i = n > C::kStages ? n - C::kStages : 0; i < n; ++i) mbar_wait(&sh->full[i % C::kStages], (i / C::kStages) & 1, attn::kDrainLimit);
+    } else if (warp == 9) {
+      // -------------------------------------------------------------------------------- products
+      constexpr uint32_t idesc = idesc_e4m3(128, TN);
+      int n = 0;
+      bool ok = true;
+      for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+        const Item w = item_of<TN>(a, idx);
+        for (int kb = w.kb0; kb < w.kb1; ++kb, ++n) {
+          const int st = n % C::kStages, buf = n % C::kBufs;
+          if (!(ok = wait(&sh->full[st], (n / C::kStages) & 1, sh, a, 10)) || !(ok = wait(&sh->acc_free[buf], ((n / C::kBufs) & 1) ^ 1, sh, a, 11))) break;
+          if (elect_one()) {
+            tc_fence_after();
+            const uint64_t da = smem_desc_kmajor(smem_u32(smem + st * C::kStage), 128), db = smem_desc_kmajor(smem_u32(smem + st * C::kStage + C::kA), 128);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mma_f8_ss(tmem + buf * TN, da + 2 * k, db + 2 * k, idesc, k > 0);
+            mma_commit(&sh->empty[st]);
+            mma_commit(&sh->acc_full[buf]);
+          }
+          __syncwarp();
+        }
+      }
+      if (elect_one()) mma_commit(&sh->drain);
+      __syncwarp();
+      mbar_wait(&sh->drain, 0, attn::kDrainLimit);
+    }
+  } else if (warp < 4 * C::kGroups) {
+    // ---------------------------------------------------------------------------------- sums
+    reg_inc<kRegAdd>();
+    constexpr int kCols = C::kCols, kChunk = kCols < 32 ? kCols : 32, kChunks = kCols / kChunk;
+    const int group = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + group * kCols;
+    int n = 0;
+    bool ok = true;
+    for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+      const Item w = item_of<TN>(a, idx);
+      uint64_t acc[kCols / 2];
+#pragma unroll
+      for (int i = 0; i < kCols / 2; ++i) acc[i] = 0;
+      const int m0 = SWAP ? w.b0 : w.a0 + row;                 // my row of x (SWAP: my columns' first)
+      const int n0 = SWAP ? w.a0 : w.b0 + group * kCols;       // my (first) weight row; all my weight rows lie in its block of 128
+      const float* wsp = a.ws + (int64_t)min(n0 >> 7, (a.N - 1) >> 7) * a.blocks;
+      // Scales of a block, fetched one block ahead: that of my row, or (SWAP) of row `lane` and 32 + lane of my columns.
+      float xa = 0.f, xb = 0.f, wv = 0.f;
+      auto fetch = [&](int kb) {
+        const float* xp = a.xs + (int64_t)kb * a.M;
+        if constexpr (SWAP) {
+          xa = m0 + lane < a.M ? __ldg(xp + m0 + lane) : 0.f;
+          if constexpr (kCols > 32) xb = m0 + 32 + lane < a.M ? __ldg(xp + m0 + 32 + lane) : 0.f;
+        } else {
+          xa = m0 < a.M ? __ldg(xp + m0) : 0.f;
+        }
+        wv = __ldg(wsp + kb);
+      };
+      fetch(w.kb0);
+      for (int kb = w.kb0; kb < w.kb1; ++kb, ++n) {
+        const int buf = n % C::kBufs;
+        const float fa = xa * wv, fb = xb * wv;
+        if (kb + 1 < w.kb1) fetch(kb + 1);
+        if (!(ok = wait(&sh->acc_full[buf], (n / C::kBufs) & 1, sh, a, 20))) break;
+        tc_fence_after();
+        const uint32_t at = lane_base + buf * TN;
+        uint32_t r[2][kChunk];
+        auto load = [&](int c) {
+          if constexpr (kChunk == 32) tmem_ld32(at + 32 * c, r[c & 1]);
+          else tmem_ld16(at, r[c & 1]);
+        };
+        load(0);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+          tmem_wait_ld();
+          if (c + 1 < kChunks) {
+            load(c + 1);
+          } else {
+            tc_fence_before();
+            mbar_arrive(&sh->acc_free[buf]);
+          }
+#pragma unroll
+          for (int i = 0; i < kChunk / 2; ++i) {
+            uint64_t f2;
+            if constexpr (SWAP) {
+              const float f = c == 0 ? fa : fb;
+              f2 = pack_f32x2(__shfl_sync(0xffffffffu, f, 2 * i), __shfl_sync(0xffffffffu, f, 2 * i + 1));
+            } else {
+              f2 = pack_f32x2(fa, fa);
+            }
+            acc[c * kChunk / 2 + i] = fma2(pack_b32x2(r[c & 1][2 * i], r[c & 1][2 * i + 1]), f2, acc[c * kChunk / 2 + i]);
+          }
+        }
+      }
+      if (!ok) break;
+      float y[kCols];
+#pragma unroll
+      for (int i = 0; i < kCols / 2; ++i) unpack2(acc[i], y[2 * i], y[2 * i + 1]);
+      const bool whole = a.splits == 1;
+      if constexpr (SWAP) {
+        const int col = w.a0 + row;
+        if (col < a.N) {
+          const float bias = whole && a.bias ? load1(a.bias, a.bias_dtype, col) : 0.f;
+#pragma unroll
+          for (int i = 0; i < kCols; ++i) {
+            if (m0 + i >= a.M) break;
+            if (!whole) a.part[((int64_t)w.split * a.M + m0 + i) * a.ldp + col] = y[i];
+            else if (a.out_dtype == VC_DTYPE_BF16) static_cast<__nv_bfloat16*>(a.out)[(m0 + i) * a.ldo + col] = __float2bfloat16_rn(y[i] + bias);
+            else if (a.out_dtype == VC_DTYPE_FP16) static_cast<__half*>(a.out)[(m0 + i) * a.ldo + col] = __float2half_rn(y[i] + bias);
+            else static_cast<float*>(a.out)[(m0 + i) * a.ldo + col] = y[i] + bias;
+          }
+        }
+      } else {
+        const int row0 = w.a0 + (warp & 3) * 32, rows = min(32, a.M - row0), cols = min(kCols, a.N - n0);
+        const uint32_t tile = smem_u32(sOut) + warp * 4096;
+        if (whole && a.bias) {
+#pragma unroll
+          for (int i = 0; i < kCols; i += 8) {
+            if (i + 8 <= cols) {
+              float b8[8];
+              load8(a.bias, a.bias_dtype, n0 + i, b8);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[i + e] += b8[e];
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (i + e < cols) y[i + e] += load1(a.bias, a.bias_dtype, n0 + i + e);
+            }
+          }
+        }
+        if (!whole) emit_rows<float, kCols>(y, tile, a.part + ((int64_t)w.split * a.M + row0) * a.ldp + n0, a.ldp, rows, cols, true, lane);
+        else if (a.out_dtype == VC_DTYPE_BF16) emit_rows<__nv_bfloat16, kCols>(y, tile, static_cast<__nv_bfloat16*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
+        else if (a.out_dtype == VC_DTYPE_FP16) emit_rows<__half, kCols>(y, tile, static_cast<__half*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
+        else emit_rows<float, kCols>(y, tile, static_cast<float*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 10) tmem_dealloc<C::kTmem>(tmem);
+}
+
+// The parts of every sum in the order of the splits, the bias, the rounding.  A thread takes four columns of a row.
+__global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant__ LinearArgs a) {
+  pdl_wait();
+  const int quads = (a.N + 3) / 4;
+  const int64_t total = (int64_t)a.M * quads;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t m = i / quads;
+    const int n = (int)(i - m * quads) * 4;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < a.splits; ++s) {
+      const float4 v = *reinterpret_cast<const float4*>(a.part + ((int64_t)s * a.M + m) * a.ldp + n);
+      y.x += v.x; y.y += v.y; y.z += v.z; y.w += v.w;
+    }
+    const float e[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (n + j >= a.N) break;
+      const float v = e[j] + (a.bias ? load1(a.bias, a.bias_dtype, n + j) : 0.f);
+      if (a.out_dtype == VC_DTYPE_BF16) static_cast<__nv_bfloat16*>(a.out)[m * a.ldo + n + j] = __float2bfloat16_rn(v);
+      else if (a.out_dtype == VC_DTYPE_FP16) static_cast<__half*>(a.out)[m * a.ldo + n + j] = __float2half_rn(v);
+      else static_cast<float*>(a.out)[m * a.ldo + n + j] = v;
+    }
+  }
+}
+
+struct Plan {
+  bool swap;
+  int tn, tiles_b, splits, blocks;
+  int64_t items, ldp;
+  size_t total;
+};
+
+vc_status resolve(const vc_linear_params* p, vc_linear_params* out, Plan* plan) {
+  if (!p) return VC_ERR_INVALID_ARG;
+  vc_linear_params r = *p;
+  if (r.M < 1 || r.N < 1 || r.M > (1 << 30) || r.N > (1 << 30) || r.K < 16 || r.K % 16 || r.K > (1 << 20)) return VC_ERR_INVALID_ARG;
+  if (bad_dtype(r.out_dtype) || bad_dtype(r.bias_dtype) || r.k_splits < 0 || r.k_splits > 64) return VC_ERR_INVALID_ARG;
+  if (r.M == 1 || r.ldx == 0) r.ldx = r.K;
+  if (r.N == 1 || r.ldw == 0) r.ldw = r.K;
+  if (r.M == 1 || r.ldo == 0) r.ldo = r.N;
+  if (r.ldx < r.K || r.ldw < r.K || r.ldo < r.N || r.ldx % 16 || r.ldw % 16 || r.ldx >= 1ll << 38 || r.ldw >= 1ll << 38 || r.ldo >= 1ll << 32) return VC_ERR_INVALID_ARG;
+  Plan pl{};
+  pl.blocks = (r.K + 127) / 128;
+  // Up to 64 rows: weights are A.  Else the wide tile where it fills the SMs, the narrow one where that has more tiles to give.
+  pl.swap = r.M <= 64;
+  const int64_t ta = pl.swap ? (r.N + 127) / 128 : (r.M + 127) / 128;
+  if (pl.swap) pl.tn = r.M <= 16 ? 16 : 64;
+  else pl.tn = ta * ((r.N + 255) / 256) >= kSms ? 256 : 128;
+  pl.tiles_b = (int)(((pl.swap ? r.M : r.N) + (int64_t)pl.tn - 1) / pl.tn);
+  const int64_t tiles = ta * pl.tiles_b;
+  pl.splits = r.k_splits;
+  if (pl.splits == 0) {
+    const int64_t room = kSms / tiles;
+    pl.splits = 1;
+    if (room > 1 && pl.blocks >= 8) pl.splits = (int)(room < pl.blocks / 4 ? room : pl.blocks / 4);
+  }
+  if (pl.splits > pl.blocks) pl.splits = pl.blocks;
+  if (pl.splits > 64) pl.splits = 64;
+  pl.items = tiles * pl.splits;
+  if (pl.items > INT32_MAX) return VC_ERR_UNSUPPORTED;
+  pl.ldp = (r.N + 3) / 4 * 4ll;
+  pl.total = 256 + (pl.splits > 1 ? (size_t)pl.splits * r.M * pl.ldp * 4 : 0);
+  *out = r;
+  *plan = pl;
+  return VC_OK;
+}
+
+bool make_map8(CUtensorMap* m, const void* base, int rows, int K, int64_t ld, int box_rows) {
+  attn::EncodeTiledFn fn = attn::encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, step[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool SWAP, int TN>
+cudaError_t launch_linear(const vc_linear_params& r, const Plan& pl, const LinearArgs& a, const void* x, const void* w, cudaStream_t s) {
+  using C = Cfg<SWAP, TN>;
+  alignas(64) CUtensorMap ta, tb;
+  if (!make_map8(&ta, SWAP ? w : x, SWAP ? r.N : r.M, r.K, SWAP ? r.ldw : r.ldx, 128) ||
+      !make_map8(&tb, SWAP ? x : w, SWAP ? r.M : r.N, r.K, SWAP ? r.ldx : r.ldw, TN))
+    return cudaErrorUnknown;
+  cudaError_t e = allow_smem<linear_fp8_kernel<SWAP, TN>>();
+  if (e != cudaSuccess) return e;
+  const int grid = pl.items < sm_count() ? (int)pl.items : sm_count();
+  constexpr size_t smem = C::kStages * C::kStage + C::kOut + sizeof(Smem<C::kStages, C::kBufs>);
+  e = launch_overlapped(linear_fp8_kernel<SWAP, TN>, dim3((unsigned)grid), kThreads, smem, s, ta, tb, a);
+  if (e != cudaSuccess) return e;
+  count_launches(1);
+  if (pl.splits > 1) {
+    const int64_t work = ((int64_t)r.M * ((r.N + 3) / 4) + 255) / 256, most = 8 * sm_count();
+    e = launch_overlapped(linear_join_kernel, dim3((unsigned)(work < most ? work : most)), 256, 0, s, a);
+    if (e != cudaSuccess) return e;
+    count_launches(1);
+  }
+  return cudaSuccess;
+}
+
+}  // namespace
+}  // namespace vc
+
+using namespace vc;
+
+extern "C" size_t vc_linear_workspace_bytes(const vc_linear_params* p) {
+  vc_linear_params r;
+  Plan pl;
+  return resolve(p, &r, &pl) == VC_OK ? pl.total : 0;
+}
+
+extern "C" vc_status vc_linear_fp8(const vc_linear_params* p, const void* x_codes, const float* x_scale, const void* w_codes, const float* w_scale,
+                                   const void* bias, void* out, void* workspace, void* stream) {
+  vc_linear_params r;
+  Plan pl;
+  const vc_status st = resolve(p, &r, &pl);
+  if (st != VC_OK) return st;
+  if (!x_codes || !x_scale || !w_codes || !w_scale || !out || !workspace) return VC_ERR_INVALID_ARG;
+  if (misaligned16(x_codes) || misaligned16(x_scale) || misaligned16(w_codes) || misaligned16(w_scale) || misaligned16(bias) || misaligned16(out) ||
+      misaligned16(workspace))
+    return VC_ERR_INVALID_ARG;
+  LinearArgs a{};
+  a.xs = x_scale; a.ws = w_scale; a.bias = bias; a.out = out;
+  a.status = (uint32_t*)workspace;
+  a.part = (float*)((uint8_t*)workspace + 256);
+  a.ldo = r.ldo; a.ldp = pl.ldp;
+  a.M = r.M; a.N = r.N; a.blocks = pl.blocks; a.tiles_b = pl.tiles_b; a.splits = pl.splits; a.items = (int)pl.items;
+  a.out_dtype = r.out_dtype; a.bias_dtype = r.bias_dtype;
+  a.vec = r.ldo * elem_size(r.out_dtype) % 16 == 0;
+  a.limit = attn::attn_wait_limit();
+  a.nonblocking = attn::attn_wait_nonblocking();
+  cudaStream_t s = (cudaStream_t)stream;
+  const cudaError_t e = pl.swap ? (pl.tn == 16 ? launch_linear<true, 16>(r, pl, a, x_codes, w_codes, s) : launch_linear<true, 64>(r, pl, a, x_codes, w_codes, s))
+                        : pl.tn == 256 ? launch_linear<false, 256>(r, pl, a, x_codes, w_codes, s)
+                                       : launch_linear<false, 128>(r, pl, a, x_codes, w_codes, s);
+  return e == cudaSuccess ? VC_OK : VC_ERR_CUDA;
+}

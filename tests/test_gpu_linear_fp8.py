@@ -1,0 +1,179 @@
+"""vc_linear_fp8 against the product in 64 bits.
+
+Tolerance per output: u |y| (its rounding, u = eps / 2 of the type) and, of the sum of the products' magnitudes, (132 + blocks + 8) 2^-24: an
+instruction adds 32 exact products and its accumulator, each term cut at no less than 24 bits below the largest (33 of them, 4
+instructions a block); each block's sum is scaled (2 roundings) and added (1 each; the parts of a split sum count among them), the bias last.
+A half value below 2^-14 lies on a grid of 2^-24 and is off by up to half of that, whatever its size: fp16 adds 2^-25.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_15810_b200 as vc
+from oracle import layer as L
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+def _operands(M, N, K, seed, spread=1.0):
+    rng = np.random.default_rng(seed)
+    nb = -(-K // 128)
+    codes = [rng.integers(0, 256, (n, K)).astype(np.uint8) for n in (M, N)]
+    for c in codes:
+        c[c & 127 == 127] = 0x30                                    # no NaN codes
+        c[rng.random(c.shape) < 0.7] &= 0xbf                        # most of them moderate
+    xs = np.exp(spread * rng.normal(size=(nb, M))).astype(np.float32)
+    ws = np.exp(spread * rng.normal(size=(-(-N // 128), nb))).astype(np.float32)
+    return codes[0], xs, codes[1], ws
+
+
+def _dev(a):
+    return torch.from_numpy(a).cuda()
+
+
+def _run(x, xs, w, ws, dt, bias=None, out=None, **kw):
+    M, N = x.shape[0], w.shape[0]
+    out = torch.full((M, N), float("nan"), dtype=DT[dt], device="cuda") if out is None else out
+    p = vc.LinearParams.of(x, w, out, bias, **kw)
+    work = torch.full((vc.vc_linear_workspace_bytes(p),), 0xff, dtype=torch.uint8, device="cuda")
+    vc.vc_linear_fp8(p, x, xs, w, ws, bias, out, work)
+    vc.vc_poll_status(work)
+    return out
+
+
+def _close(got, x, xs, w, ws, dt, bias=None):
+    want, size = L.linear_fp8(x, xs, w, ws, None if bias is None else bias.double().cpu().numpy())
+    blocks = xs.shape[0]
+    tol = torch.finfo(DT[dt]).eps / 2 * np.abs(want) + (132 + blocks + 8) * 2.0 ** -24 * size
+    if dt == "fp16":
+        tol = tol + 2.0 ** -25
+    err = np.abs(got.double().cpu().numpy() - want)
+    assert (err <= tol).all(), f"{(~(err <= tol)).sum()} of {err.size} off, worst {np.nanmax(err / tol):.2f}"
+
+
+def _check(M, N, K, dt="bf16", bias=True, bias_dt=None, seed=1, **kw):
+    x, xs, w, ws = _operands(M, N, K, seed + M + 3 * N + 7 * K)
+    b = torch.randn(N, generator=torch.Generator().manual_seed(seed)).mul(100.0).to(DT[bias_dt or dt]).cuda() if bias else None
+    if dt == "fp16":                                                # keep the outputs inside the type's range
+        xs, ws = xs * np.float32(2.0 ** -8), ws * np.float32(2.0 ** -8)
+    out = _run(_dev(x), _dev(xs), _dev(w), _dev(ws), dt, b, **kw)
+    _close(out, x, xs, w, ws, dt, b)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 129, 128), (16, 128, 256), (17, 64, 144), (64, 300, 1024), (65, 1, 16), (100, 130, 272), (128, 256, 128),
+                                   (129, 257, 400), (300, 513, 640)])
+def test_sizes_and_types(dt, M, N, K):
+    _check(M, N, K, dt)
+    _check(M, N, K, dt, bias=False)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 640, 5120), (7, 200, 2048), (40, 384, 1536), (200, 136, 2176), (130, 260, 4096)])
+@pytest.mark.parametrize("splits", [0, 1, 2, 5, 64])
+def test_sums_split_between_ctas(M, N, K, splits):
+    _check(M, N, K, "bf16", k_splits=splits)
+    _check(M, N, K, "fp32", bias_dt="bf16", k_splits=splits)
+
+
+@pytest.mark.parametrize("N", [2560, 2570, 2433])
+def test_wide_tiles(N):
+    """Enough tiles of 128 x 256 for every SM, several a CTA; widths whose rows of outputs are and are not on 16-byte boundaries."""
+    _check(2500, N, 256, "bf16")
+    _check(2500, N, 144, "fp32", bias_dt="fp16")
+
+
+@pytest.mark.parametrize("M", [5, 50, 200, 2500])
+def test_rows_of_wider_matrices_and_neighbours(M):
+    N, K = 2500, 160
+    x, xs, w, ws = _operands(M, N, K, 5)
+    wide_x, wide_w = np.full((M, K + 32), 0x7f, np.uint8), np.full((N, K + 48), 0x7f, np.uint8)      # NaN codes around
+    wide_x[:, 16:16 + K], wide_w[:, 16:16 + K] = x, w
+    room = torch.full((M + 2, N + 11), 7.0, dtype=torch.float32, device="cuda")
+    for pad in (4, 8):
+        out = room[1:M + 1, pad:pad + N] if pad == 4 else torch.full((M + 2, N + 12), 7.0, device="cuda")[1:M + 1, 4:4 + N]
+        if out.data_ptr() % 16:
+            continue
+        _run(_dev(wide_x)[:, 16:16 + K], _dev(xs), _dev(wide_w)[:, 16:16 + K], _dev(ws), "fp32", None, out)
+        _close(out, x, xs, w, ws, "fp32")
+    assert (room[0] == 7).all() and (room[M + 1] == 7).all()
+
+
+def test_scales_far_apart_and_zero():
+    x, xs, w, ws = _operands(90, 140, 1024, 8, spread=6.0)
+    xs[3], ws[0, 5] = 0.0, 0.0
+    _close(_run(_dev(x), _dev(xs), _dev(w), _dev(ws), "fp32"), x, xs, w, ws, "fp32")
+
+
+@pytest.mark.parametrize("M", [4, 200])
+def test_nan_and_infinite_scales_stay_in_their_rows(M):
+    x, xs, w, ws = _operands(M, 150, 512, 9)
+    xs[1, 2] = np.nan
+    x[3, 200] = 0x7f
+    out = _run(_dev(x), _dev(xs), _dev(w), _dev(ws), "fp32").cpu()
+    bad = torch.zeros(M, dtype=torch.bool)
+    bad[2] = bad[3] = True
+    assert torch.isnan(out[bad]).all() and torch.isfinite(out[~bad]).all()
+
+
+def test_codes_as_quantised_and_as_float8_tensors():
+    """Quantised by the library and multiplied: the product of what the codes stand for."""
+    g = torch.Generator().manual_seed(10)
+    x, w = torch.randn(70, 400, generator=g).to(torch.bfloat16).cuda(), torch.randn(200, 400, generator=g).cuda()
+    out = []
+    for t, rows in ((x, 1), (w, 128)):
+        codes = torch.empty(t.shape, dtype=torch.float8_e4m3fn, device="cuda")
+        scale = torch.empty((4, 70) if rows == 1 else (2, 4), device="cuda")
+        vc.vc_quant_fp8(vc.QuantParams.of(t, rows), t, codes, scale)
+        out += [codes, scale]
+    y = _run(*out, "fp32")
+    c = [t.view(torch.uint8).cpu().numpy() if t.dtype == torch.float8_e4m3fn else t.cpu().numpy() for t in out]
+    _close(y, *c, "fp32")
+    # two roundings of at most 2^-4 relative (or half the least step of a block, 2^-10 of 448) each
+    ref, size = x.double() @ w.double().t(), x.double().abs() @ w.double().abs().t()
+    assert ((y.double() - ref).abs() <= 0.13 * size + 1.0).all()
+
+
+@pytest.mark.parametrize("M", [3, 300])
+def test_same_answer_other_stream_and_captured(M):
+    x, xs, w, ws = (_dev(t) for t in _operands(M, 400, 4096, 11))
+    want = _run(x, xs, w, ws, "bf16")
+    assert torch.equal(_run(x, xs, w, ws, "bf16"), want)
+    out = torch.empty_like(want)
+    p = vc.LinearParams.of(x, w, out)
+    work = torch.empty(vc.vc_linear_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)
+        vc.vc_poll_status(work)
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)
+    xs.mul_(2.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, _run(x, xs, w, ws, "bf16"))
+
+
+@pytest.mark.parametrize("M,N", [(3, 400), (40, 400), (300, 400), (2500, 2560)])
+def test_wait_that_runs_out_is_reported_and_leaves_the_library_usable(M, N):
+    x, xs, w, ws = (_dev(t) for t in _operands(M, N, 1024, 12))
+    want = _run(x, xs, w, ws, "bf16")
+    out = torch.empty_like(want)
+    p = vc.LinearParams.of(x, w, out)
+    work = torch.empty(vc.vc_linear_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    try:
+        vc.vc_test_set_wait_limit(1)
+        vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)
+        with pytest.raises(vc.VcError) as e:
+            vc.vc_poll_status(work)
+        assert e.value.code == vc.VC_ERR_TIMEOUT
+    finally:
+        vc.vc_test_set_wait_limit(0)
+    vc.vc_poll_status(work)
+    vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)
+    vc.vc_poll_status(work)
+    assert torch.equal(out, want)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2609_15810_b200 as vc
-from paper_2609_15810_b200.binding import CrossParams, QkParams, QuantParams, Strides
+from paper_2609_15810_b200.binding import CrossParams, LinearParams, QkParams, QuantParams, Strides
 
 P = 4096          # stands for an aligned address: a refused call never looks at it
 
@@ -101,8 +101,41 @@ def test_cross_attn_workspace():
     assert size() >= 256 and size(N_q=100000) == 256             # enough rows: nothing to split
 
 
+def _linear(ptrs=(P,) * 7, **kw):
+    p = LinearParams(M=5, N=6, K=32)
+    for n, val in kw.items():
+        setattr(p, n, val)
+    return vc.load_library().vc_linear_fp8(ctypes.byref(p), *ptrs, None), vc.vc_linear_workspace_bytes(p)
+
+
+@pytest.mark.parametrize("kw", [dict(M=0), dict(N=0), dict(K=0), dict(K=24), dict(K=(1 << 20) + 16), dict(M=(1 << 30) + 1), dict(N=(1 << 30) + 1), dict(out_dtype=3),
+                                dict(bias_dtype=-1), dict(k_splits=-1), dict(k_splits=65), dict(ldx=16), dict(ldx=40), dict(ldw=-32), dict(ldo=5),
+                                dict(ldo=1 << 32)])
+def test_linear_fp8_parameters(kw):
+    assert _linear(**kw) == (vc.VC_ERR_INVALID_ARG, 0)
+
+
+@pytest.mark.parametrize("at", range(7))
+def test_linear_fp8_pointers(at):
+    for bad in (P + 8, None):
+        ptrs = [P] * 7
+        ptrs[at] = bad
+        if not (at == 4 and bad is None):                        # (no bias is no mistake)
+            assert _linear(ptrs)[0] == vc.VC_ERR_INVALID_ARG
+
+
+def test_linear_fp8_workspace():
+    def size(M, N, K, splits=0):
+        return vc.vc_linear_workspace_bytes(LinearParams(M=M, N=N, K=K, k_splits=splits))
+    assert size(1, 5120, 5120, 1) == 256
+    assert size(1, 5120, 5120, 3) == 256 + 3 * 5120 * 4
+    assert size(2, 5, 512, 64) == 256 + 4 * 2 * 8 * 4            # no more splits than blocks; rows of a part padded to 16 bytes
+    assert size(32760, 5120, 5120) == 256
+
+
 def test_no_parameters():
     lib = vc.load_library()
+    assert lib.vc_linear_fp8(None, P, P, P, P, P, P, P, None) == vc.VC_ERR_INVALID_ARG and lib.vc_linear_workspace_bytes(None) == 0
     assert lib.vc_cross_attn(None, P, P, P, P, P, P, P, P, None) == vc.VC_ERR_INVALID_ARG and lib.vc_cross_workspace_bytes(None) == 0
     assert lib.vc_qk_norm_rope(None, P, P, P, P, P, P, P, None) == vc.VC_ERR_INVALID_ARG
     assert lib.vc_quant_fp8(None, P, P, P, None) == vc.VC_ERR_INVALID_ARG
@@ -130,4 +163,5 @@ def test_sizes_of_the_parameter_blocks():
     assert ctypes.sizeof(Strides) == 24
     assert ctypes.sizeof(QkParams) == 22 * 4 + 8 * 4 + 4 * 24
     assert ctypes.sizeof(CrossParams) == 8 * 4 + 4 + 4 + 4 * 24          # 4 bytes of padding in front of the strides, as in C
+    assert ctypes.sizeof(LinearParams) == 6 * 4 + 3 * 8
     assert ctypes.sizeof(QuantParams) == 6 * 4 + 24
