@@ -84,9 +84,9 @@ class Strides(ctypes.Structure):
         """Of a [B, H, N, d] tensor in elements; its channels have to lie side by side."""
         if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
             raise ValueError("a [B, H, N, d] tensor with d contiguous is wanted")
-        # strides of dimensions of one entry say nothing; all zero would mean packed
-        n = t.stride(2) if t.shape[2] > 1 else t.shape[3]
-        return cls(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0, n)
+        if t.shape[2] > 1 and t.stride(2) == 0:
+            raise ValueError("rows that share one address: a [B, H, N, d] tensor with tokens apart is wanted")
+        return cls(t.stride(0), t.stride(1), t.stride(2) or t.shape[3])         # (all zero would mean packed)
 
 
 class QkParams(ctypes.Structure):
@@ -247,8 +247,13 @@ def _ptr(t):
     return t.data_ptr()
 
 
+# The current stream's handle.  torch.cuda.current_stream() builds an object around it, 3 us of a small call's 10; PyTorch's own
+# generated code asks for the number alone.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _check(code, where):
@@ -389,99 +394,134 @@ def _types(code):
     return (_TORCH[code],)
 
 
-def _tensor(name, t, device, dtypes, shape=None, strides=None):
-    """The address of a tensor of the operators around the attention.  These take tensors of several types and layouts, so the
-    binding compares them with what the parameter block says: the C entry sees addresses alone.  `strides` None: contiguous."""
+# The operators around the attention take tensors of several types and layouts, and the C entry sees addresses alone, so the binding
+# compares the tensors with what the parameter block says.  What a block asks of each argument, (name, types, shape, strides), is
+# derived from its bytes once: reading it from the structure field by field cost 7 of a call's 20 us of host time.
+_wants = {}
+
+
+def _wanted(p, derive):
+    key = (derive, bytes(p))
+    got = _wants.get(key)
+    if got is None:
+        if len(_wants) >= 4096:
+            _wants.clear()
+        got = _wants[key] = derive(p)
+    return got
+
+
+def _packed(shape):
+    out, n = [], 1
+    for s in reversed(shape):
+        out.append(n)
+        n *= s
+    return tuple(reversed(out))
+
+
+def _head_want(name, code, shape, s):
+    """A [B, H, N, d] tensor under the vc_strides of the parameter block."""
+    return (name, _types(code), shape, (s.b, s.h, s.n, 1) if s.b or s.h or s.n else _packed(shape))
+
+
+def _want(name, types, shape):
+    return (name, types, shape, _packed(shape))
+
+
+def _address(t, device, want):
     if t is None:
         return None
+    name, types, shape, strides = want
     if t.get_device() != device:
         raise ValueError(f"{name}: on {t.device}, and the current device is cuda:{device}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name}: {t.dtype}, not {' or '.join(str(d) for d in dtypes)}")
-    if shape is not None and t.shape != shape:
+    if t.dtype not in types:
+        raise ValueError(f"{name}: {t.dtype}, not {' or '.join(str(d) for d in types)}")
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, not {shape}")
-    if strides is None:
-        if not t.is_contiguous():
-            raise ValueError(f"{name}: has to be contiguous")
-    elif t.stride() != strides and any(n > 1 and i != w for n, i, w in zip(t.shape, t.stride(), strides)):
-        raise ValueError(f"{name}: strides {t.stride()}, not {strides} as in the parameters")
+    if t.stride() != strides:          # (a dimension of one entry may have any)
+        for n, got, wanted in zip(shape, t.stride(), strides):
+            if n > 1 and got != wanted:
+                raise ValueError(f"{name}: strides {t.stride()}, not {strides}")
     return t.data_ptr()
 
 
-def _heads(name, t, device, dtypes, shape, s):
-    """The same for a [B, H, N, d] tensor under the vc_strides of the parameter block."""
-    b, h, n = s.b, s.h, s.n
-    _, H, N, d = shape
-    return _tensor(name, t, device, dtypes, shape, (b, h, n, 1) if b or h or n else (H * N * d, N * d, d, 1))
+def _workspace(t, device, need, where):
+    if need == 0:
+        raise VcError(VC_ERR_INVALID_ARG, where)
+    if t is None:
+        return None
+    if t.get_device() != device or t.dtype != torch.uint8 or not t.is_contiguous():
+        raise ValueError(f"workspace: contiguous uint8 on cuda:{device} is wanted")
+    if t.numel() < need:
+        raise ValueError(f"workspace: {t.numel()} bytes, not {need}")
+    return t.data_ptr()
+
+
+def _qk_wants(p):
+    qs, ks = (p.B, p.H_q, p.N, p.d), (p.B, p.H_k, p.N, p.d)
+    wt, heads = _types(p.weight_dtype), p.norm == VC_NORM_TOKEN
+    return (_head_want("q", p.dtype, qs, p.q), _head_want("k", p.dtype, ks, p.k), _want("q_weight", wt, (p.d * (p.H_q if heads else 1),)),
+            _want("k_weight", wt, (p.d * (p.H_k if heads else 1),)), _want("positions", _INT32, (p.B, p.N, 3)),
+            _head_want("q_out", p.dtype, qs, p.q_out), _head_want("k_out", p.dtype, ks, p.k_out))
 
 
 def vc_qk_norm_rope(p, q, k, q_weight, k_weight, positions, q_out, k_out):
-    """RMS norm (p.norm) and rotation (p.rotary) of q and k into q_out and k_out; q, k, a weight or positions may be None."""
-    lib, dev, dt, wt = load_library(), torch.cuda.current_device(), _types(p.dtype), _types(p.weight_dtype)
-    qs, ks = (p.B, p.H_q, p.N, p.d), (p.B, p.H_k, p.N, p.d)
-    heads = p.norm == VC_NORM_TOKEN
-    _check(lib.vc_qk_norm_rope(ctypes.byref(p), _heads("q", q, dev, dt, qs, p.q), _heads("k", k, dev, dt, ks, p.k),
-                               _weight("q_weight", q_weight, dev, wt, p.d * (p.H_q if heads else 1)),
-                               _weight("k_weight", k_weight, dev, wt, p.d * (p.H_k if heads else 1)),
-                               _tensor("positions", positions, dev, _INT32, (p.B, p.N, 3)),
-                               _heads("q_out", q_out, dev, dt, qs, p.q_out), _heads("k_out", k_out, dev, dt, ks, p.k_out), _stream()),
-           "vc_qk_norm_rope")
-
-
-def _weight(name, t, device, dtypes, count):
-    if t is not None and t.numel() != count:
-        raise ValueError(f"{name}: {t.numel()} elements, not {count}")
-    return _tensor(name, t, device, dtypes)
+    """RMS norm (p.norm) and rotation (p.rotary) of q and k into q_out and k_out; q, k, a weight [d] or [H d], or positions may be None."""
+    dev, w = torch.cuda.current_device(), _wanted(p, _qk_wants)
+    _check(load_library().vc_qk_norm_rope(ctypes.byref(p), _address(q, dev, w[0]), _address(k, dev, w[1]), _address(q_weight, dev, w[2]),
+                                          _address(k_weight, dev, w[3]), _address(positions, dev, w[4]), _address(q_out, dev, w[5]),
+                                          _address(k_out, dev, w[6]), _stream()), "vc_qk_norm_rope")
 
 
 def vc_cross_workspace_bytes(p):
     return int(load_library().vc_cross_workspace_bytes(ctypes.byref(p)))
 
 
-def _workspace(t, device, need, where):
-    if need == 0:
-        raise VcError(VC_ERR_INVALID_ARG, where)
-    if t is not None and t.numel() < need:
-        raise ValueError(f"workspace: {t.numel()} bytes, not {need}")
-    return _tensor("workspace", t, device, _BYTES)
+def _cross_wants(p):
+    qs, ks = (p.B, p.H, p.N_q, p.d), (p.B, p.H_kv, p.N_kv, p.d)
+    return (_head_want("q", p.dtype, qs, p.q), _head_want("k", p.dtype, ks, p.k), _head_want("v", p.dtype, ks, p.v), _want("kv_len", _INT32, (p.B,)),
+            _want("key_mask", _MASK, (p.B, p.N_kv)), _head_want("o", p.dtype, qs, p.o), _want("lse", _FP32, (p.B, p.H, p.N_q)), vc_cross_workspace_bytes(p))
 
 
 def vc_cross_attn(p, q, k, v, kv_len, key_mask, o, lse, workspace):
     """o = softmax(scale q k^T over the kept keys) v; kv_len int32 [B], key_mask bool or uint8 [B, N_kv] and lse fp32 [B, H, N_q] may be None."""
-    lib, dev, dt = load_library(), torch.cuda.current_device(), _types(p.dtype)
-    qs, ks = (p.B, p.H, p.N_q, p.d), (p.B, p.H_kv, p.N_kv, p.d)
-    _check(lib.vc_cross_attn(ctypes.byref(p), _heads("q", q, dev, dt, qs, p.q), _heads("k", k, dev, dt, ks, p.k), _heads("v", v, dev, dt, ks, p.v),
-                             _tensor("kv_len", kv_len, dev, _INT32, (p.B,)), _tensor("key_mask", key_mask, dev, _MASK, (p.B, p.N_kv)),
-                             _heads("o", o, dev, dt, qs, p.o), _tensor("lse", lse, dev, _FP32, (p.B, p.H, p.N_q)),
-                             _workspace(workspace, dev, vc_cross_workspace_bytes(p), "vc_cross_attn"), _stream()), "vc_cross_attn")
+    dev, w = torch.cuda.current_device(), _wanted(p, _cross_wants)
+    _check(load_library().vc_cross_attn(ctypes.byref(p), _address(q, dev, w[0]), _address(k, dev, w[1]), _address(v, dev, w[2]),
+                                        _address(kv_len, dev, w[3]), _address(key_mask, dev, w[4]), _address(o, dev, w[5]), _address(lse, dev, w[6]),
+                                        _workspace(workspace, dev, w[7], "vc_cross_attn"), _stream()), "vc_cross_attn")
+
+
+def _quant_wants(p):
+    rows, cols = p.B * p.N, p.H * p.d
+    nb = (cols + 127) // 128
+    x = _head_want("x", p.dtype, (p.B, p.H, p.N, p.d), p.x)
+    return (x, (x[0], x[1], x[2][2:], x[3][2:]) if p.B == p.H == 1 else x, _want("codes", _CODES, (rows, cols)),
+            _want("scale", _FP32, (nb, rows) if p.block_rows == 1 else ((rows + 127) // 128, nb)))
 
 
 def vc_quant_fp8(p, x, codes, scale):
     """E4M3 codes [B N, H d] (float8_e4m3fn or uint8) and FP32 scales of x, [B, H, N, d] or a matrix [rows, columns]."""
-    lib, dev = load_library(), torch.cuda.current_device()
-    rows, cols = p.B * p.N, p.H * p.d
-    nb = (cols + 127) // 128
-    _check(lib.vc_quant_fp8(ctypes.byref(p), _heads("x", x if x.dim() == 4 else x[None, None], dev, _types(p.dtype), (p.B, p.H, p.N, p.d), p.x),
-                            _tensor("codes", codes, dev, _CODES, (rows, cols)),
-                            _tensor("scale", scale, dev, _FP32, (nb, rows) if p.block_rows == 1 else ((rows + 127) // 128, nb)), _stream()),
-           "vc_quant_fp8")
+    dev, w = torch.cuda.current_device(), _wanted(p, _quant_wants)
+    _check(load_library().vc_quant_fp8(ctypes.byref(p), _address(x, dev, w[0] if x.dim() == 4 else w[1]), _address(codes, dev, w[2]),
+                                       _address(scale, dev, w[3]), _stream()), "vc_quant_fp8")
 
 
 def vc_linear_workspace_bytes(p):
     return int(load_library().vc_linear_workspace_bytes(ctypes.byref(p)))
 
 
+def _linear_wants(p):
+    nb = (p.K + 127) // 128
+    return (("x_codes", _CODES, (p.M, p.K), (p.ldx or p.K, 1)), _want("x_scale", _FP32, (nb, p.M)), ("w_codes", _CODES, (p.N, p.K), (p.ldw or p.K, 1)),
+            _want("w_scale", _FP32, ((p.N + 127) // 128, nb)), _want("bias", _types(p.bias_dtype), (p.N,)),
+            ("out", _types(p.out_dtype), (p.M, p.N), (p.ldo or p.N, 1)), vc_linear_workspace_bytes(p))
+
+
 def vc_linear_fp8(p, x_codes, x_scale, w_codes, w_scale, bias, out, workspace):
     """out = x w^T + bias from codes and scales as vc_quant_fp8 writes them (x with block_rows 1, w with 128); bias [N] or None."""
-    lib, dev = load_library(), torch.cuda.current_device()
-    nb = (p.K + 127) // 128
-    _check(lib.vc_linear_fp8(ctypes.byref(p), _tensor("x_codes", x_codes, dev, _CODES, (p.M, p.K), (p.ldx or p.K, 1)),
-                             _tensor("x_scale", x_scale, dev, _FP32, (nb, p.M)),
-                             _tensor("w_codes", w_codes, dev, _CODES, (p.N, p.K), (p.ldw or p.K, 1)),
-                             _tensor("w_scale", w_scale, dev, _FP32, ((p.N + 127) // 128, nb)),
-                             _tensor("bias", bias, dev, _types(p.bias_dtype), (p.N,)),
-                             _tensor("out", out, dev, _types(p.out_dtype), (p.M, p.N), (p.ldo or p.N, 1)),
-                             _workspace(workspace, dev, vc_linear_workspace_bytes(p), "vc_linear_fp8"), _stream()), "vc_linear_fp8")
+    dev, w = torch.cuda.current_device(), _wanted(p, _linear_wants)
+    _check(load_library().vc_linear_fp8(ctypes.byref(p), _address(x_codes, dev, w[0]), _address(x_scale, dev, w[1]), _address(w_codes, dev, w[2]),
+                                        _address(w_scale, dev, w[3]), _address(bias, dev, w[4]), _address(out, dev, w[5]),
+                                        _workspace(workspace, dev, w[6], "vc_linear_fp8"), _stream()), "vc_linear_fp8")
 
 
 def vc_launch_count():

@@ -8,6 +8,7 @@
 
 #include "vc_internal.h"
 #include "vc_launch.h"
+#include "vc_sm100.cuh"
 
 namespace vc {
 namespace layer {
@@ -54,6 +55,7 @@ template <> __device__ __forceinline__ uint32_t pack16<__half>(float a, float b)
 template <typename T> struct Raw8 {
   uint4 v;
   __device__ __forceinline__ void load(const T* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void load_again(const T* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }     // (read by many CTAs)
   __device__ __forceinline__ void get(float (&f)[8]) const {
     const float2 a = unpack16<T>(v.x), b = unpack16<T>(v.y), c = unpack16<T>(v.z), d = unpack16<T>(v.w);
     f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
@@ -65,6 +67,10 @@ template <> struct Raw8<float> {
   __device__ __forceinline__ void load(const float* p) {
     a = __ldcs(reinterpret_cast<const float4*>(p));
     b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void load_again(const float* p) {
+    a = __ldg(reinterpret_cast<const float4*>(p));
+    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
   }
   __device__ __forceinline__ void get(float (&f)[8]) const {
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
@@ -78,6 +84,15 @@ template <> __device__ __forceinline__ void store8<float>(float* p, const float 
   reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
   reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
 }
+// f times a number, f times g, two products an instruction.
+__device__ __forceinline__ void times(float (&f)[8], float g) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) sm100::unpack2(sm100::mul2(sm100::pack_f32x2(f[e], f[e + 1]), sm100::pack_f32x2(g, g)), f[e], f[e + 1]);
+}
+__device__ __forceinline__ void times(float (&f)[8], const float (&g)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) sm100::unpack2(sm100::mul2(sm100::pack_f32x2(f[e], f[e + 1]), sm100::pack_f32x2(g[e], g[e + 1])), f[e], f[e + 1]);
+}
 // One element / eight elements of an array whose type is an argument.
 __device__ __forceinline__ float load1(const void* p, int dtype, int64_t i) {
   if (dtype == VC_DTYPE_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
@@ -90,12 +105,8 @@ __device__ __forceinline__ void load8(const void* p, int dtype, int64_t i, float
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
   } else {
     const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i));
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 t = dtype == VC_DTYPE_BF16 ? unpack16<__nv_bfloat16>(w[j]) : unpack16<__half>(w[j]);
-      f[2 * j] = t.x; f[2 * j + 1] = t.y;
-    }
+    if (dtype == VC_DTYPE_BF16) Raw8<__nv_bfloat16>{u}.get(f);
+    else Raw8<__half>{u}.get(f);
   }
 }
 #endif

@@ -13,15 +13,21 @@ namespace {
 
 using namespace layer;
 
-constexpr int kThreads = 256, kKeep = 8, kMaxPairs = 128, kBatch = 4;
+constexpr int kThreads = 256, kMaxPairs = 128;
+
+// Heads whose channels a thread holds in registers: three CTAs an SM then fit the register file.
+__host__ __device__ constexpr int heads_held(int elem_bytes, int rotary) { return (elem_bytes == 2 ? 8 : 4) / (rotary == VC_ROTARY_HALF ? 2 : 1); }
 
 struct QkArgs {
   const void *x[2], *w[2];
   void* y[2];
   const int32_t* positions;
   vc_strides in[2], out[2];
-  int H[2];
-  int N, tiles, chunks, log_lanes, log_hl, weight_dtype;
+  int H[2], first;                 // first: 1 if there is no Q
+  int N, chunks, log_lanes, log_hl, log_pairs, weight_dtype;     // log_pairs: 2^log_pairs >= pairs
+  int turns_taken;                 // a CTA takes that many groups of tokens, one behind the other
+  bool same_type;                  // weights are of the tensors' type
+  bool partial;                    // some channels are not rotated
   int pairs, pair_end[3];          // rotated pairs; where each axis's pairs end
   int grid_h, grid_w, start[3];
   float eps, inv_count[2], mult;
@@ -31,9 +37,12 @@ struct QkArgs {
 // Angles of the CTA's tokens.  The product is formed in FP64: in FP32 the angle of position 10^5 is off by 10^-2.
 // Whole turns are taken off there too, and sincospi sees |x| <= 1.
 __device__ __forceinline__ void fill_table(const QkArgs& a, float2* tab, int b, int n0, int tokens) {
-  for (int i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
-    const int tt = i / a.pairs, p = i - tt * a.pairs, n = min(n0 + tt, a.N - 1);
-    const int axis = (p >= a.pair_end[0]) + (p >= a.pair_end[1]);
+  const int p = threadIdx.x & ((1 << a.log_pairs) - 1);
+  if (p >= a.pairs) return;
+  const int axis = (p >= a.pair_end[0]) + (p >= a.pair_end[1]);
+  const double turns = a.turns[p];
+  for (int tt = threadIdx.x >> a.log_pairs; tt < tokens; tt += kThreads >> a.log_pairs) {
+    const int n = min(n0 + tt, a.N - 1);
     int pos;
     if (a.positions) {
       pos = a.positions[((int64_t)b * a.N + n) * 3 + axis];
@@ -41,172 +50,203 @@ __device__ __forceinline__ void fill_table(const QkArgs& a, float2* tab, int b, 
       const int row = n / a.grid_w;
       pos = a.start[axis] + (axis == 2 ? n - row * a.grid_w : axis == 1 ? row % a.grid_h : row / a.grid_h);
     }
-    const double t = (double)pos * a.turns[p];
+    const double t = (double)pos * turns;
     float s, c;
     sincospif(2.0f * (float)(t - rint(t)), &s, &c);
-    tab[i] = make_float2(c * a.mult, s * a.mult);
+    tab[tt * a.pairs + p] = make_float2(c * a.mult, s * a.mult);
   }
 }
 
-template <typename T, int NORM, int ROT>
-__global__ void __launch_bounds__(kThreads)
-qk_norm_kernel(const __grid_constant__ QkArgs a) {
-  extern __shared__ float2 tab[];                       // [tokens][pairs]
-  __shared__ float xch[ROT == VC_ROTARY_HALF ? kThreads * 8 : 1];
-  __shared__ float part[NORM == VC_NORM_TOKEN ? kThreads : 1];
-  const int lanes = 1 << a.log_lanes, hls = 1 << a.log_hl, rows = kThreads >> a.log_lanes, tokens = rows >> a.log_hl;
-  const int c = threadIdx.x & (lanes - 1), r = threadIdx.x >> a.log_lanes, hl = r & (hls - 1), tt = r >> a.log_hl;
-  const int b = blockIdx.x / a.tiles, n0 = (blockIdx.x - b * a.tiles) * tokens, n = n0 + tt;
-  const bool live = n < a.N && c < a.chunks;
-  pdl_wait();
-  // cos and sin of my channels; where a channel is not rotated, bit e of `still` is set
-  constexpr int kAngles = ROT == VC_ROTARY_HALF ? 8 : 4;
-  float cs[kAngles], sn[kAngles];
-  int src[ROT == VC_ROTARY_HALF ? 8 : 1];
-  uint32_t still = 0;
-  if constexpr (ROT != VC_ROTARY_NONE) {
-    fill_table(a, tab, b, n0, tokens);
-    __syncthreads();
-    const float2* mine = tab + tt * a.pairs;
-#pragma unroll
-    for (int e = 0; e < kAngles; ++e) {
-      cs[e] = 1.f; sn[e] = 0.f;
-      if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
-        const int p = 4 * c + e;
-        if (p < a.pairs) { cs[e] = mine[p].x; sn[e] = mine[p].y; } else still |= 1u << e;
-      } else {
-        const int ch = 8 * c + e;
-        src[e] = e * lanes + c;
-        if (ch < 2 * a.pairs) {
-          const int axis = (ch >= 2 * a.pair_end[0]) + (ch >= 2 * a.pair_end[1]);
-          const int p0 = axis ? a.pair_end[axis - 1] : 0, half = a.pair_end[axis] - p0, i = ch - 2 * p0;
-          const bool low = i < half;
-          const int other = low ? ch + half : ch - half;
-          const float2 t = mine[p0 + (low ? i : i - half)];
-          cs[e] = t.x; sn[e] = low ? -t.y : t.y;
-          src[e] = (other & 7) * lanes + (other >> 3);
-        } else {
-          still |= 1u << e;
-        }
-      }
-    }
+// f times eight weights.  Their type is an argument; as a rule it is the tensors'.
+template <typename T> __device__ __forceinline__ void times_weights(float (&f)[8], const QkArgs& a, const void* w, int64_t at) {
+  float wt[8];
+  if (a.same_type) {
+    Raw8<T> raw;
+    raw.load_again(static_cast<const T*>(w) + at);
+    raw.get(wt);
+  } else {
+    load8(w, a.weight_dtype, at, wt);
   }
-  auto rotate = [&](float (&f)[8]) {
-    if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float f0 = f[2 * e], f1 = f[2 * e + 1];
-        const bool keep = still >> e & 1;
-        f[2 * e] = keep ? f0 : f0 * cs[e] - f1 * sn[e];
-        f[2 * e + 1] = keep ? f1 : f0 * sn[e] + f1 * cs[e];
-      }
-    } else if constexpr (ROT == VC_ROTARY_HALF) {
-      // a pair's halves are half an axis apart, in another lane as a rule: the head's channels change places in
-      // shared memory, element-major so that the lanes of an access lie side by side
-      float* row = xch + r * 8 * lanes;
-      __syncwarp();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) row[e * lanes + c] = f[e];
-      __syncwarp();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float g = row[src[e]];
-        f[e] = still >> e & 1 ? f[e] : f[e] * cs[e] + g * sn[e];
-      }
-    }
-  };
-  auto lanes_sum = [&](float v) {
-    for (int s = lanes >> 1; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
+  times(f, wt);
+}
+
+template <typename T, int NORM, int ROT>
+__global__ void __launch_bounds__(kThreads, 3)
+qk_norm_kernel(const __grid_constant__ QkArgs a) {
+  extern __shared__ float2 tab[];                       // [tokens of the CTA][pairs]
+  __shared__ float xch[ROT == VC_ROTARY_HALF ? kThreads * 8 + 1 : 1];   // (the last one is 0)
+  __shared__ float part[2][NORM == VC_NORM_TOKEN ? kThreads / 32 : 1];
+  constexpr int kKeep = heads_held(sizeof(T), ROT);
+  const int lanes = 1 << a.log_lanes, tokens = kThreads >> (a.log_lanes + a.log_hl);
+  const int c = threadIdx.x & (lanes - 1), r = threadIdx.x >> a.log_lanes, hl = r & ((1 << a.log_hl) - 1), tt = r >> a.log_hl;
+  const int b = blockIdx.y, n0 = blockIdx.x * tokens * a.turns_taken;
+  const int t = blockIdx.z + a.first, H = a.H[t];       // Q or K
+  const void* w = a.w[t];
+  // My heads are hl, hl + hls, ...: kKeep of them are loaded at a time.  (A thread without a token or a channel reads the last
+  // one's and stores nothing.)
+  const int64_t sx = a.in[t].h << a.log_hl, sy = a.out[t].h << a.log_hl, xn = a.in[t].n;
+  const T* xb = static_cast<const T*>(a.x[t]) + (b * a.in[t].b + 8 * min(c, a.chunks - 1));
+  T* yb = static_cast<T*>(a.y[t]) + (b * a.out[t].b + hl * a.out[t].h + (int64_t)(n0 + tt) * a.out[t].n + 8 * c);
+  const int64_t w_at0 = ((int64_t)hl * a.chunks + min(c, a.chunks - 1)) * 8;
+
+  auto lanes_sum = [](float v, int count) {
+    for (int s = count >> 1; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
     return v;
   };
-  auto squares = [](const Raw8<T>& raw) {
-    float f[8], s = 0.f;
-    raw.get(f);
+  auto squares = [](const Raw8<T>& v) {
+    float f[8], even, odd;
+    uint64_t s = 0;
+    v.get(f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(f[e], f[e], s);
-    return s;
+    for (int e = 0; e < 8; e += 2) {
+      const uint64_t f2 = sm100::pack_f32x2(f[e], f[e + 1]);
+      s = sm100::fma2(f2, f2, s);
+    }
+    sm100::unpack2(s, even, odd);
+    return even + odd;
   };
+  float wt[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) wt[e] = 1.f;
+  if (NORM == VC_NORM_HEAD && w && c < a.chunks) times_weights<T>(wt, a, w, 8 * c);
 
-#pragma unroll 1
-  for (int t = 0; t < 2; ++t) {
-    const int H = a.H[t];
-    if (H == 0) continue;
-    const T* x = static_cast<const T*>(a.x[t]) + b * a.in[t].b + (int64_t)n * a.in[t].n + 8 * c;
-    T* y = static_cast<T*>(a.y[t]) + b * a.out[t].b + (int64_t)n * a.out[t].n + 8 * c;
-    const int64_t sh = a.in[t].h, oh = a.out[t].h;
-    const void* w = a.w[t];
-    float wt[8];
+  pdl_wait();
+  // The angles of all tokens at once: every lane has one to form.  The first tokens' heads are on their way meanwhile.
+  Raw8<T> raw[kKeep];
+  auto load_heads = [&](int n, int h0) {
+    const T* x0 = xb + (int64_t)min(n, a.N - 1) * xn;
+    const T* from = x0 + hl * a.in[t].h + (h0 >> a.log_hl) * sx;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) wt[e] = 1.f;
+    for (int i = 0; i < kKeep; ++i) {
+      const int h = h0 + (i << a.log_hl);
+      if (h >= H) break;
+      raw[i].load(h + hl < H ? from : x0);
+      from += sx;
+    }
+  };
+  load_heads(n0 + tt, 0);
+  if constexpr (ROT != VC_ROTARY_NONE) fill_table(a, tab, b, n0, tokens * a.turns_taken);
+  if (ROT == VC_ROTARY_HALF && threadIdx.x == 0) xch[kThreads * 8] = 0.f;
+  if constexpr (ROT != VC_ROTARY_NONE && NORM != VC_NORM_TOKEN) __syncthreads();
+
+  for (int turn = 0; turn < a.turns_taken; ++turn) {
+    const int n = n0 + turn * tokens + tt;
+    if (n - tt >= a.N) break;
+    const bool live = n < a.N && c < a.chunks;
+    if (turn) load_heads(n, 0);
+    float inv = 1.f;
     if constexpr (NORM == VC_NORM_TOKEN) {
-      Raw8<T> raw[kKeep];
       float ss = 0.f;
+      for (int h0 = 0;;) {
 #pragma unroll
-      for (int i = 0; i < kKeep; ++i) {
-        const int h = hl + (i << a.log_hl);
-        raw[i].zero();
-        if (live && h < H) raw[i].load(x + h * sh);
-      }
-#pragma unroll
-      for (int i = 0; i < kKeep; ++i) ss += squares(raw[i]);
-      for (int h = hl + (kKeep << a.log_hl); h < H; h += hls) {      // more heads than the registers hold: read twice
-        Raw8<T> more;
-        more.zero();
-        if (live) more.load(x + h * sh);
-        ss += squares(more);
-      }
-      ss = lanes_sum(ss);
-      __syncthreads();                                               // (the sums of Q have been read)
-      if (c == 0) part[r] = ss;
-      __syncthreads();
-      float sum = 0.f;
-      for (int i = 0; i < hls; ++i) sum += part[tt * hls + i];       // one order for every thread of the token
-      const float inv = rsqrtf(fmaf(sum, a.inv_count[t], a.eps));
-      auto finish = [&](const Raw8<T>& v, int h) {
-        float f[8];
-        v.get(f);
-        if (w && live && h < H) load8(w, a.weight_dtype, ((int64_t)h * a.chunks + c) * 8, wt);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = f[e] * inv * wt[e];
-        rotate(f);
-        if (live && h < H) store8<T>(y + h * oh, f);
-      };
-#pragma unroll
-      for (int i = 0; i < kKeep; ++i)
-        if ((i << a.log_hl) < H) finish(raw[i], hl + (i << a.log_hl));
-      for (int h0 = kKeep << a.log_hl; h0 < H; h0 += hls) {
-        Raw8<T> more;
-        more.zero();
-        if (live && h0 + hl < H) more.load(x + (h0 + hl) * sh);
-        finish(more, h0 + hl);
-      }
-    } else {
-      if (NORM == VC_NORM_HEAD && w && c < a.chunks) load8(w, a.weight_dtype, 8 * c, wt);
-      const int step = hls * gridDim.y;
-      for (int h0 = blockIdx.y * hls; h0 < H; h0 += kBatch * step) {
-        Raw8<T> raw[kBatch];
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const int h = h0 + i * step + hl;
-          raw[i].zero();
-          if (live && h < H) raw[i].load(x + h * sh);
+        for (int i = 0; i < kKeep; ++i) {
+          const int h = h0 + (i << a.log_hl);
+          if (h >= H) break;
+          const float sq = squares(raw[i]);
+          ss += h + hl < H ? sq : 0.f;
         }
+        h0 += kKeep << a.log_hl;
+        if (h0 >= H) break;
+        load_heads(n, h0);
+      }
+      if (c >= a.chunks) ss = 0.f;
+      ss = lanes_sum(ss, min(lanes << a.log_hl, 32));                    // a token's lanes in this warp
+      if ((threadIdx.x & 31) == 0) part[turn & 1][threadIdx.x >> 5] = ss;
+      __syncthreads();
+      const int warps = lanes << a.log_hl >> 5;                          // of a token; 0 or 1: its sum is at hand
+      if (warps > 1) {
+        ss = 0.f;
+        for (int i = 0; i < warps; ++i) ss += part[turn & 1][(threadIdx.x >> 5 & -warps) + i];   // one order for every thread of the token
+      }
+      inv = rsqrtf(fmaf(ss, a.inv_count[t], a.eps));
+      if (H > kKeep << a.log_hl) load_heads(n, 0);                       // more heads than the registers hold: read twice
+    }
+
+    // cos and sin of my channels.  One that is not rotated keeps its value whatever its neighbour holds: bit e of `still`, or 0 in the
+    // place of the other half (with eight bits to test the predicate registers run out).
+    constexpr int kAngles = ROT == VC_ROTARY_HALF ? 8 : 4;
+    float cs[kAngles], sn[kAngles];
+    int src[ROT == VC_ROTARY_HALF ? 8 : 1];
+    uint32_t still = 0;
+    if constexpr (ROT != VC_ROTARY_NONE) {
+      const float2* mine = tab + (turn * tokens + tt) * a.pairs;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const int h = h0 + i * step + hl;
-          if (h0 + i * step >= H) break;
-          float f[8];
-          raw[i].get(f);
-          if constexpr (NORM == VC_NORM_HEAD) {
-            const float inv = rsqrtf(fmaf(lanes_sum(squares(raw[i])), a.inv_count[t], a.eps));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = f[e] * inv * wt[e];
+      for (int e = 0; e < kAngles; ++e) {
+        cs[e] = 1.f; sn[e] = 0.f;
+        if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
+          const int p = 4 * c + e;
+          if (p < a.pairs) { cs[e] = mine[p].x; sn[e] = mine[p].y; } else still |= 1u << e;
+        } else {
+          const int ch = 8 * c + e;
+          src[e] = kThreads * 8 - r * 8 * lanes;
+          if (ch < 2 * a.pairs) {
+            const int axis = (ch >= 2 * a.pair_end[0]) + (ch >= 2 * a.pair_end[1]);
+            const int p0 = axis ? a.pair_end[axis - 1] : 0, half = a.pair_end[axis] - p0, i = ch - 2 * p0;
+            const bool low = i < half;
+            const int other = low ? ch + half : ch - half;
+            const float2 cosine_sine = mine[p0 + (low ? i : i - half)];
+            cs[e] = cosine_sine.x; sn[e] = low ? -cosine_sine.y : cosine_sine.y;
+            src[e] = (other & 7) * lanes + (other >> 3);
           }
-          rotate(f);
-          if (live && h < H) store8<T>(y + h * oh, f);
         }
       }
     }
+    auto rotate = [&](float (&f)[8]) {
+      if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
+        float g[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          g[2 * e] = f[2 * e] * cs[e] - f[2 * e + 1] * sn[e];
+          g[2 * e + 1] = f[2 * e] * sn[e] + f[2 * e + 1] * cs[e];
+        }
+        if (a.partial) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (still >> (e / 2) & 1) g[e] = f[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = g[e];
+      } else if constexpr (ROT == VC_ROTARY_HALF) {
+        // a pair's halves are half an axis apart, in another lane as a rule: the head's channels change places in
+        // shared memory, element-major so that the lanes of an access lie side by side
+        float* row = xch + r * 8 * lanes;
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) row[e * lanes + c] = f[e];
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = f[e] * cs[e] + row[src[e]] * sn[e];
+      }
+    };
+
+    T* y = yb;
+    int64_t w_at = w_at0;
+    for (int h0 = 0; h0 < H;) {
+#pragma unroll
+      for (int i = 0; i < kKeep; ++i) {
+        const int h = h0 + (i << a.log_hl);
+        if (h >= H) break;
+        const bool mine = live && h + hl < H;
+        float f[8];
+        raw[i].get(f);
+        if constexpr (NORM == VC_NORM_HEAD) {
+          const float sq = squares(raw[i]);
+          times(f, rsqrtf(fmaf(lanes_sum(c < a.chunks ? sq : 0.f, lanes), a.inv_count[t], a.eps)));
+          times(f, wt);
+        }
+        if constexpr (NORM == VC_NORM_TOKEN) {
+          times(f, inv);
+          if (w && mine) times_weights<T>(f, a, w, w_at);
+          w_at += (int64_t)a.chunks * 8 << a.log_hl;
+        }
+        rotate(f);
+        if (mine) store8<T>(y, f);
+        y += sy;
+      }
+      h0 += kKeep << a.log_hl;
+      if (h0 < H) load_heads(n, h0);
+    }
+    yb += tokens * a.out[t].n;
   }
 }
 
@@ -279,6 +319,7 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
       {p->H_q, q, q_weight, q_out, &p->q, &p->q_out}, {p->H_k, k, k_weight, k_out, &p->k, &p->k_out}};
   for (int t = 0; t < 2; ++t) {
     a.H[t] = side[t].H;
+    a.inv_count[t] = 1.0f / ((float)p->d * (p->norm == VC_NORM_TOKEN && side[t].H ? side[t].H : 1));
     if (side[t].H == 0) continue;
     if (!side[t].x || !side[t].y || misaligned16(side[t].x) || misaligned16(side[t].y) || misaligned16(side[t].w)) return VC_ERR_INVALID_ARG;
     if (!resolve_strides(*side[t].in, p->B, side[t].H, p->N, p->d, es, false, &a.in[t]) ||
@@ -287,7 +328,6 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
     if (side[t].x == side[t].y && (a.in[t].b != a.out[t].b || a.in[t].h != a.out[t].h || a.in[t].n != a.out[t].n)) return VC_ERR_INVALID_ARG;
     a.x[t] = side[t].x; a.y[t] = side[t].y;
     a.w[t] = p->norm == VC_NORM_NONE ? nullptr : side[t].w;
-    a.inv_count[t] = 1.0f / ((float)p->d * (p->norm == VC_NORM_TOKEN ? side[t].H : 1));
   }
   int rot = p->rotary;
   if (rot != VC_ROTARY_NONE) {
@@ -331,26 +371,26 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
   }
   a.N = p->N;
   a.chunks = p->d / 8;
+  a.same_type = p->weight_dtype == p->dtype;
+  a.partial = 2 * a.pairs < p->d;
   a.weight_dtype = p->weight_dtype;
   a.eps = p->eps != 0.f ? p->eps : 1e-6f;
   while ((1 << a.log_lanes) < a.chunks) ++a.log_lanes;
-  const int rows = kThreads >> a.log_lanes, heads = a.H[0] > a.H[1] ? a.H[0] : a.H[1];
+  const int rows = kThreads >> a.log_lanes, heads = a.H[0] > a.H[1] ? a.H[0] : a.H[1], keep = heads_held(es, rot);
+  const int tensors = (a.H[0] > 0) + (a.H[1] > 0);
+  a.first = a.H[0] == 0;
+  while ((1 << a.log_pairs) < a.pairs) ++a.log_pairs;
   // Rows of a CTA side by side: `1 << log_hl` heads of each token.  The norm over a token takes as many as bring the heads that
-  // a thread keeps down to kKeep; else as many as a short sequence leaves without a token.
-  if (p->norm == VC_NORM_TOKEN)
-    while ((1 << a.log_hl) < rows && (heads > kKeep << a.log_hl || (rows >> a.log_hl) >= 2 * p->N)) ++a.log_hl;
-  else
-    while ((1 << a.log_hl) < rows && (rows >> a.log_hl) >= 2 * p->N) ++a.log_hl;
-  const int tokens = rows >> a.log_hl;
-  a.tiles = (p->N + tokens - 1) / tokens;
-  const int64_t ctas = (int64_t)p->B * a.tiles;
-  if (ctas > INT32_MAX) return VC_ERR_UNSUPPORTED;
-  int split = 1;
-  if (p->norm != VC_NORM_TOKEN) {            // few tokens: their heads go to several CTAs
-    const int64_t most = (heads + (1 << a.log_hl) - 1) >> a.log_hl, want = (8 * sm_count() + ctas - 1) / ctas;
-    split = (int)(want < most ? want : most);
-  }
-  const dim3 grid((unsigned)ctas, (unsigned)split);
+  // a thread holds down to `keep`; beyond that as many as leave four CTAs an SM, or a short sequence without a token.
+  auto ctas = [&] { return (int64_t)p->B * tensors * ((p->N + (rows >> a.log_hl) - 1) / (rows >> a.log_hl)); };
+  while ((1 << a.log_hl) < rows && ((p->norm == VC_NORM_TOKEN && heads > keep << a.log_hl) || (heads >= 2 << a.log_hl && ctas() < 4 * sm_count()) ||
+                                    (rows >> a.log_hl) >= 2 * p->N))
+    ++a.log_hl;
+  // Several groups of tokens a CTA where that leaves every SM its share: addresses and angles are formed for all of them at once.
+  a.turns_taken = 1;
+  while (a.turns_taken < 8 && ctas() >= 16 * a.turns_taken * sm_count() && (2 * a.turns_taken * (rows >> a.log_hl)) * a.pairs <= 1024) a.turns_taken *= 2;
+  const int tokens = (rows >> a.log_hl) * a.turns_taken, tiles = (p->N + tokens - 1) / tokens;
+  const dim3 grid((unsigned)tiles, (unsigned)p->B, (unsigned)tensors);
   const size_t smem = rot == VC_ROTARY_NONE ? 0 : (size_t)tokens * a.pairs * sizeof(float2);
   cudaStream_t s = (cudaStream_t)stream;
   const cudaError_t e = p->dtype == VC_DTYPE_BF16   ? launch_norm<__nv_bfloat16>(p->norm, rot, a, grid, smem, s)
