@@ -1,8 +1,8 @@
 // vc_cross_attn: attention of queries to an encoder's keys and values, at 16 bits on the tensor cores.
 //
 // A persistent CTA works through items: one or two 128-row query tiles of a head against the head's key tiles (128 keys each), or a
-// part of them.  Warps 0-3 and 4-7 are the softmax of the two query tiles, 8-11 the epilogue, 12 loads, 13 issues the
-// products, 14 clears value rows of masked keys.
+// part of them.  Warps 0-3 and 4-7 are the softmax of the two query tiles, 8-11 the epilogue, 12 loads keys and
+// values, 13 issues the products, 14 clears value rows of masked keys, 15 loads queries.
 //
 //   S_t = Q_t K^T    both operands in shared memory, K-major, FP32 accumulators in 128 columns of tensor memory
 //   P_t = 2^(s S_t - m)  in registers, a thread per row; written back as 16-bit values over S_t's own columns
@@ -98,6 +98,11 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* m, uin
       : "memory");
 }
 
+__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* m, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+               : "memory");
+}
+
 // MN-major operand in the 128-byte swizzle: rows of 64 channels of one key, 8 keys a kilobyte, the next 64 channels a panel on.
 __device__ __forceinline__ uint64_t desc_mnmajor(uint32_t saddr, uint32_t panel_bytes) {
   return (uint64_t)((saddr & 0x3FFFF) >> 4) | (uint64_t)(panel_bytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
@@ -119,9 +124,9 @@ template <int D> struct Lay {
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                  const __grid_constant__ CrossArgs a) {
+                  const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ CrossArgs a) {
   using L = Lay<D>;
-  constexpr int kRegSoftmax = 184, kRegEpi = 104, kRegCtl = 40;
+  constexpr int kRegSoftmax = 176, kRegEpi = 104, kRegCtl = 56;
   static_assert(2 * kRegSoftmax + kRegEpi + kRegCtl <= 4 * 128, "register budget exceeds the CTA's allocation");
   static_assert(L::kSmem <= 227 * 1024, "shared memory of the kernel exceeds the SM");
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -158,12 +163,11 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     reg_dec<kRegCtl>();
     if (warp == 12) {
       // -------------------------------------------------------------------------------- loads
-      int g = 0, n[2] = {0, 0};                     // key tiles; items of each query tile
+      int g = 0;                                    // key tiles
       int issued = 0;                               // ring slots filled
       bool ok = true;
       auto fill = [&](const CUtensorMap* m, int row, int ch, int cb) {
         const int st = issued % kStages;
-        if (!(ok = wait(&sh->empty[st], ((issued / kStages) & 1) ^ 1, sh, a, 1))) return;
         if (elect_one()) {
           mbar_expect_tx(&sh->full[st], L::kTile);
           for (int c = 0; c < D / 64; ++c) tma_load_4d(sKV + st * L::kTile + c * kPanel, m, &sh->full[st], 64 * c, row, ch, cb);
@@ -171,13 +175,12 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         __syncwarp();
         ++issued;
       };
+      auto room = [&] { return ok = wait(&sh->empty[issued % kStages], ((issued / kStages) & 1) ^ 1, sh, a, 1); };
       for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
         const Item w = item_of(a, idx);
-        if (w.nt == 0) continue;
         const int hk = w.h / a.group;
-        for (int j = 0; ok && j < w.nt; ++j, ++g) {
+        for (int j = 0; j < w.nt; ++j, ++g) {
           const int row = (w.t0 + j) * 128;
-          // the slot's last readers are four key tiles back, and this tile's copy waits for the keys of two tiles back
           uint32_t words[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -186,30 +189,47 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             if (a.key_mask && keep) keep = __ldg(a.key_mask + (int64_t)w.b * a.Nkv + key) != 0;
             words[i] = __ballot_sync(0xffffffffu, keep);
           }
-          if (!(ok = wait(&sh->empty[issued % kStages], ((issued / kStages) & 1) ^ 1, sh, a, 2))) break;
+          if (!room()) break;
+          // (the words' last readers are four key tiles back, and this slot's keys were read two tiles back)
           if (lane < 4) sh->bits[g & 3][lane] = lane == 0 ? words[0] : lane == 1 ? words[1] : lane == 2 ? words[2] : words[3];
           __syncwarp();
           fill(&tm_k, row, hk * a.k_h, w.b * a.k_b);
-          if (!ok) break;
-          if (j == 0) {
-            for (int t = 0; ok && t < (w.two ? 2 : 1); ++t, ++n[t - 1]) {
-              if (!(ok = wait(&sh->q_free[t], (n[t] & 1) ^ 1, sh, a, 3))) break;
-              if (elect_one()) {
-                mbar_expect_tx(&sh->q_full[t], L::kTile);
-                for (int c = 0; c < D / 64; ++c)
-                  tma_load_4d(sQ + t * L::kTile + c * kPanel, &tm_q, &sh->q_full[t], 64 * c, (w.q0 + t) * 128, w.h * a.q_h, w.b * a.q_b);
-              }
-              __syncwarp();
-            }
-            if (!ok) break;
-          }
+          if (!room()) break;
           fill(&tm_v, row, hk * a.v_h, w.b * a.v_b);
         }
       }
       // every copy issued has landed before the CTA may end (at once on a normal run)
+      for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(&sh->full[i % kStages], (i / kStages) & 1, attn::kDrainLimit);
+    } else if (warp == 15) {
+      // -------------------------------------------------------------------------------- queries
+      // A warp of their own: a query tile waits for its predecessor's last product, and keys must not wait behind it.  The next
+      // item's queries are fetched into L2 meanwhile.
+      int n[2] = {0, 0};
+      bool ok = true;
+      for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+        const Item w = item_of(a, idx);
+        if (w.nt > 0) {
+          for (int t = 0; t < (w.two ? 2 : 1); ++t) {
+            if (!(ok = wait(&sh->q_free[t], (n[t] & 1) ^ 1, sh, a, 3))) break;
+            if (elect_one()) {
+              mbar_expect_tx(&sh->q_full[t], L::kTile);
+              for (int c = 0; c < D / 64; ++c)
+                tma_load_4d(sQ + t * L::kTile + c * kPanel, &tm_q, &sh->q_full[t], 64 * c, (w.q0 + t) * 128, w.h * a.q_h, w.b * a.q_b);
+            }
+            __syncwarp();
+            ++n[t];
+          }
+        }
+        if (ok && idx + (int)gridDim.x < a.items) {
+          const Item x = item_of(a, idx + gridDim.x);
+          if (x.nt > 0 && elect_one())
+            for (int t = 0; t < (x.two ? 2 : 1); ++t)
+              for (int c = 0; c < D / 64; ++c) tma_prefetch_4d(&tm_q, 64 * c, (x.q0 + t) * 128, x.h * a.q_h, x.b * a.q_b);
+          __syncwarp();
+        }
+      }
       for (int t = 0; t < 2; ++t)
         if (n[t]) mbar_wait(&sh->q_full[t], (n[t] - 1) & 1, attn::kDrainLimit);
-      for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(&sh->full[i % kStages], (i / kStages) & 1, attn::kDrainLimit);
     } else if (warp == 13) {
       // -------------------------------------------------------------------------------- products
       constexpr uint32_t idesc_s = idesc16<T>(128, 128), idesc_o = idesc16<T>(128, D) | (1u << 16);
@@ -457,21 +477,24 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           continue;
         }
         if (a.lse && lane < rows) a.lse[line] = lse2 * kLn2;
-        T* dst = static_cast<T*>(a.o) + w.b * a.so.b + w.h * a.so.h + (int64_t)row0 * a.so.n;
 #pragma unroll
         for (int half = 0; half < D / 64; ++half) {
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");          // the copy in front has read the rows
+          __syncwarp();
 #pragma unroll
           for (int c = 0; c < 8; ++c) sts128(Out::chunk(tile, lane, c), out[32 * half + 4 * c], out[32 * half + 4 * c + 1], out[32 * half + 4 * c + 2], out[32 * half + 4 * c + 3]);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int r = 4 * k + (lane >> 3), c = lane & 7;
-            if (r < rows) *reinterpret_cast<float4*>(dst + r * a.so.n + 64 * half + 8 * c) = lds128(Out::chunk(tile, r, c));
+          if (lane == 0 && rows > 0) {                 // (rows behind the last query are left as they are)
+            asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(reinterpret_cast<uint64_t>(&tm_o)), "r"(tile),
+                         "r"(64 * half), "r"(row0), "r"(w.h), "r"(w.b)
+                         : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
-          __syncwarp();
         }
       }
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // the rows have left before the CTA may end
   }
   tc_fence_before();
   __syncthreads();
@@ -534,8 +557,9 @@ vc_status resolve(const vc_cross_params* p, vc_cross_params* out, Plan* plan) {
   pl.rows = (int64_t)r.B * r.H * r.N_q;
   pl.qtiles = (r.N_q + 127) / 128;
   const int64_t bh = (int64_t)r.B * r.H;
-  // Two query tiles an item share the keys' copies; with fewer pairs than SMs the tiles go to CTAs of their own.
-  pl.tiles_per_item = bh * ((pl.qtiles + 1) / 2) >= kSms ? 2 : 1;
+  // Two query tiles an item share the keys' copies and keep the tensor cores busy in turn; a pair takes about 1.3 times a tile alone.
+  // With so few pairs that twice as many tiles still fit the SMs, every tile has a CTA of its own.
+  pl.tiles_per_item = 2 * bh * ((pl.qtiles + 1) / 2) > kSms ? 2 : 1;
   pl.qitems = (pl.qtiles + pl.tiles_per_item - 1) / pl.tiles_per_item;
   const int ktiles = (r.N_kv + 127) / 128;
   pl.splits = r.key_splits;
@@ -557,31 +581,32 @@ vc_status resolve(const vc_cross_params* p, vc_cross_params* out, Plan* plan) {
   return VC_OK;
 }
 
-// [B][H][N][d] of 16-bit elements, boxes of 64 channels x 128 rows in the 128-byte swizzle.  A broadcast dimension becomes one
+// [B][H][N][d] of 16-bit elements, boxes of 64 channels x `box_rows` in the 128-byte swizzle.  A broadcast dimension becomes one
 // entry (its coordinate is multiplied by 0).
-bool make_map16(CUtensorMap* m, const void* base, const vc_strides& s, int B, int H, int N, int d, int* mul_b, int* mul_h) {
+bool make_map16(CUtensorMap* m, const void* base, const vc_strides& s, int B, int H, int N, int d, int box_rows, int* mul_b, int* mul_h) {
   attn::EncodeTiledFn fn = attn::encode_fn();
   if (!fn) return false;
   *mul_b = s.b != 0; *mul_h = s.h != 0;
   const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)N, (cuuint64_t)(s.h ? H : 1), (cuuint64_t)(s.b ? B : 1)};
   const cuuint64_t strides[3] = {(cuuint64_t)s.n * 2, (cuuint64_t)(s.h ? s.h : s.n) * 2, (cuuint64_t)(s.b ? s.b : s.n) * 2};
-  const cuuint32_t box[4] = {64, 128, 1, 1}, step[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, step[4] = {1, 1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int D>
 cudaError_t launch_cross(const vc_cross_params& r, const Plan& pl, CrossArgs& a, const void* q, const void* k, const void* v, cudaStream_t s) {
-  alignas(64) CUtensorMap tq, tk, tv;
+  alignas(64) CUtensorMap tq, tk, tv, to;
   const bool any = r.N_kv > 0;                      // without keys nothing is loaded, and any valid map will do
-  if (!make_map16(&tq, q, r.q, r.B, r.H, r.N_q, D, &a.q_b, &a.q_h)) return cudaErrorUnknown;
+  int one_b, one_h;
+  if (!make_map16(&tq, q, r.q, r.B, r.H, r.N_q, D, 128, &a.q_b, &a.q_h) || !make_map16(&to, a.o, r.o, r.B, r.H, r.N_q, D, 32, &one_b, &one_h)) return cudaErrorUnknown;
   tk = tv = tq;
-  if (any && (!make_map16(&tk, k, r.k, r.B, r.H_kv, r.N_kv, D, &a.k_b, &a.k_h) || !make_map16(&tv, v, r.v, r.B, r.H_kv, r.N_kv, D, &a.v_b, &a.v_h)))
+  if (any && (!make_map16(&tk, k, r.k, r.B, r.H_kv, r.N_kv, D, 128, &a.k_b, &a.k_h) || !make_map16(&tv, v, r.v, r.B, r.H_kv, r.N_kv, D, 128, &a.v_b, &a.v_h)))
     return cudaErrorUnknown;
   cudaError_t e = allow_smem<cross_attn_kernel<T, D>>();
   if (e != cudaSuccess) return e;
   const int grid = pl.items < sm_count() ? (int)pl.items : sm_count();
-  e = launch_overlapped(cross_attn_kernel<T, D>, dim3((unsigned)grid), kThreads, Lay<D>::kSmem, s, tq, tk, tv, a);
+  e = launch_overlapped(cross_attn_kernel<T, D>, dim3((unsigned)grid), kThreads, Lay<D>::kSmem, s, tq, tk, tv, to, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
   if (pl.splits > 1) {
