@@ -1,11 +1,11 @@
 // vc_cross_attn: attention of queries to an encoder's keys and values, at 16 bits on the tensor cores.
 //
 // A persistent CTA works through items: one or two 128-row query tiles of a head against the head's key tiles (128 keys each), or a
-// part of them.  Warps 0-3 and 4-7 are the softmax of the two query tiles, 8-11 the epilogue, 12 loads keys and
-// values, 13 issues the products, 14 clears value rows of masked keys, 15 loads queries.
+// part of them.  Warp 0 loads, 1 and 3 issue the products of the two query tiles, 2 clears value rows of masked keys; 4-7 and
+// 8-11 are the softmax of the two query tiles, 12-15 the epilogue.
 //
 //   S_t = Q_t K^T    both operands in shared memory, K-major, FP32 accumulators in 128 columns of tensor memory
-//   P_t = 2^(s S_t - m)  in registers, a thread per row; written back as 16-bit values over S_t's own columns
+//   P_t = 2^(s S_t - m)  in registers, a thread a row; written back as 16-bit values over S_t's own columns
 //   O_t += P_t V     P_t from tensor memory, V as it was loaded ([key][channel], read MN-major)
 //
 // The running maximum m of a row is a reference, not the exact maximum: O_t and the row sum are rescaled only when a tile
@@ -13,8 +13,13 @@
 // so a rescale is rare, and the softmax warps do it themselves: S_t(j) complete says that the product of tile j - 1,
 // issued in front of it, is complete too.
 //
-// Bound by the tensor cores and the special-function unit together: a pair of tiles of 128 keys takes 2048 cycles of either at
-// d = 128 (4 products of 512 cycles; 32768 exponentials, 16 a cycle).
+// What bounds it: per query tile the chain S_t -> softmax (1900 cycles) -> O_t product and next S_t (1024 at d = 128, 1300 with the
+// hand-overs), two of which overlap; a pair of tiles of 128 keys takes 3500 cycles, where the tensor cores need
+// 2048.  B1 H40 32760 x 512 d128 320 us (1075 TFLOP/s), 8192 x 4096 577 us (1190).  Tried and slower there: one warp that issues
+// for both tiles 332 us (its waits and descriptors lie between the products; 567 at 4096 keys), two that do not take turns (both tiles in the same phase),
+// the turn passed at half of a tile's scores 344, two threads a row and 24 warps 358, a polynomial for one exponential in 8 / 4 / 3: 344 / 360 / 372,
+// scores read twice from tensor memory instead of held in registers 363 (650 at 4096), the second half of P handed over on its own 343,
+// exponentials in front of the tile's maximum 433.  Output rows by TMA instead of by the epilogue's own stores: 403 -> 363.
 #include <cmath>
 #include <type_traits>
 
@@ -49,7 +54,7 @@ struct CrossArgs {
 
 struct Smem {
   uint64_t full[kStages], empty[kStages], fixed[2];
-  uint64_t q_full[2], q_free[2], s_full[2], p_full[2], o_full[2], o_free[2], drain;
+  uint64_t q_full[2], q_free[2], s_full[2], p_full[2], o_full[2], o_free[2], turn[2], drain[2];
   alignas(16) uint32_t bits[4][4];                // kept keys of a tile
   float2 ml[2][2][128];                           // [a tile's items in turn][query tile][row]: reference, row sum
   uint32_t tmem_base;
@@ -98,11 +103,6 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* m, uin
       : "memory");
 }
 
-__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* m, int c0, int c1, int c2, int c3) {
-  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-               : "memory");
-}
-
 // MN-major operand in the 128-byte swizzle: rows of 64 channels of one key, 8 keys a kilobyte, the next 64 channels a panel on.
 __device__ __forceinline__ uint64_t desc_mnmajor(uint32_t saddr, uint32_t panel_bytes) {
   return (uint64_t)((saddr & 0x3FFFF) >> 4) | (uint64_t)(panel_bytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ CrossArgs a) {
   using L = Lay<D>;
-  constexpr int kRegSoftmax = 176, kRegEpi = 104, kRegCtl = 56;
+  constexpr int kRegSoftmax = 176, kRegEpi = 80, kRegCtl = 80;
   static_assert(2 * kRegSoftmax + kRegEpi + kRegCtl <= 4 * 128, "register budget exceeds the CTA's allocation");
   static_assert(L::kSmem <= 227 * 1024, "shared memory of the kernel exceeds the SM");
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -138,20 +138,20 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   const bool masked = a.kv_len || a.key_mask;       // some value row may have to be cleared
 
   if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 1); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 2); }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(&sh->fixed[t], 1);
+      mbar_init(&sh->fixed[t], 1); mbar_init(&sh->turn[t], 1);
       mbar_init(&sh->q_full[t], 1); mbar_init(&sh->q_free[t], 1);
       mbar_init(&sh->s_full[t], 1); mbar_init(&sh->p_full[t], 128);
       mbar_init(&sh->o_full[t], 1); mbar_init(&sh->o_free[t], 128);
     }
-    mbar_init(&sh->drain, 1);
+    mbar_init(&sh->drain[0], 1); mbar_init(&sh->drain[1], 1);
     sh->abort = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tm_q); tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v);
   }
   pdl_wait();
-  if (warp == 14) { tmem_alloc<512>(&sh->tmem_base); tmem_relinquish(); }
+  if (warp == 2) { tmem_alloc<512>(&sh->tmem_base); tmem_relinquish(); }
   if (tid == 0 && blockIdx.x == 0) *a.status = 0;
   tc_fence_before();
   __syncthreads();
@@ -159,12 +159,12 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   const uint32_t tmem = sh->tmem_base;
   const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
 
-  if (warp >= 12) {
+  if (warp < 4) {
     reg_dec<kRegCtl>();
-    if (warp == 12) {
+    if (warp == 0) {
       // -------------------------------------------------------------------------------- loads
       int g = 0;                                    // key tiles
-      int issued = 0;                               // ring slots filled
+      int issued = 0, n[2] = {0, 0};                // ring slots filled, query tiles loaded
       bool ok = true;
       auto fill = [&](const CUtensorMap* m, int row, int ch, int cb) {
         const int st = issued % kStages;
@@ -194,123 +194,123 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           if (lane < 4) sh->bits[g & 3][lane] = lane == 0 ? words[0] : lane == 1 ? words[1] : lane == 2 ? words[2] : words[3];
           __syncwarp();
           fill(&tm_k, row, hk * a.k_h, w.b * a.k_b);
+          if (j == 0) {                             // queries, each tile's when its predecessor's last scores are complete
+            for (int t = 0; t < (w.two ? 2 : 1); ++t) {
+              if (!(ok = wait(&sh->q_free[t], (n[t] & 1) ^ 1, sh, a, 3))) break;
+              if (elect_one()) {
+                mbar_expect_tx(&sh->q_full[t], L::kTile);
+                for (int c = 0; c < D / 64; ++c)
+                  tma_load_4d(sQ + t * L::kTile + c * kPanel, &tm_q, &sh->q_full[t], 64 * c, (w.q0 + t) * 128, w.h * a.q_h, w.b * a.q_b);
+              }
+              __syncwarp();
+              ++n[t];
+            }
+            if (!ok) break;
+          }
           if (!room()) break;
           fill(&tm_v, row, hk * a.v_h, w.b * a.v_b);
         }
       }
-      // every copy issued has landed before the CTA may end (at once on a normal run)
-      for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(&sh->full[i % kStages], (i / kStages) & 1, attn::kDrainLimit);
-    } else if (warp == 15) {
-      // -------------------------------------------------------------------------------- queries
-      // A warp of their own: a query tile waits for its predecessor's last product, and keys must not wait behind it.  The next
-      // item's queries are fetched into L2 meanwhile.
-      int n[2] = {0, 0};
-      bool ok = true;
-      for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
-        const Item w = item_of(a, idx);
-        if (w.nt > 0) {
-          for (int t = 0; t < (w.two ? 2 : 1); ++t) {
-            if (!(ok = wait(&sh->q_free[t], (n[t] & 1) ^ 1, sh, a, 3))) break;
-            if (elect_one()) {
-              mbar_expect_tx(&sh->q_full[t], L::kTile);
-              for (int c = 0; c < D / 64; ++c)
-                tma_load_4d(sQ + t * L::kTile + c * kPanel, &tm_q, &sh->q_full[t], 64 * c, (w.q0 + t) * 128, w.h * a.q_h, w.b * a.q_b);
-            }
-            __syncwarp();
-            ++n[t];
-          }
-        }
-        if (ok && idx + (int)gridDim.x < a.items) {
-          const Item x = item_of(a, idx + gridDim.x);
-          if (x.nt > 0 && elect_one())
-            for (int t = 0; t < (x.two ? 2 : 1); ++t)
-              for (int c = 0; c < D / 64; ++c) tma_prefetch_4d(&tm_q, 64 * c, (x.q0 + t) * 128, x.h * a.q_h, x.b * a.q_b);
-          __syncwarp();
-        }
-      }
       for (int t = 0; t < 2; ++t)
         if (n[t]) mbar_wait(&sh->q_full[t], (n[t] - 1) & 1, attn::kDrainLimit);
-    } else if (warp == 13) {
-      // -------------------------------------------------------------------------------- products
+      // every copy issued has landed before the CTA may end (at once on a normal run)
+      for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(&sh->full[i % kStages], (i / kStages) & 1, attn::kDrainLimit);
+    } else if (warp == 1 || warp == 3) {
+      // -------------------------------------------------------------------------------- products, one warp a query tile
+      // (with one warp for both, each group of products began 200 cycles behind the end of the one in front)
       constexpr uint32_t idesc_s = idesc16<T>(128, 128), idesc_o = idesc16<T>(128, D) | (1u << 16);
-      struct Pos { int idx, j, g; Item w; };
-      Pos cur{(int)blockIdx.x - (int)gridDim.x, 0, 0, {}};
-      auto next = [&](Pos& p) {                     // to the next key tile; false behind the last one
-        if (++p.j < p.w.nt) { ++p.g; return true; }
-        do {
-          p.idx += gridDim.x;
-          if (p.idx >= a.items) return false;
-          p.w = item_of(a, p.idx);
-        } while (p.w.nt == 0);
-        p.j = 0;
-        ++p.g;
-        return true;
-      };
-      cur.g = -1;
-      int nq[2] = {0, 0}, no[2] = {0, 0}, np[2] = {0, 0};       // uses of Q_t, O_t, P_t
+      const int t = warp >> 1;
+      const uint32_t s_at = tmem + 128 * t, o_at = tmem + L::kO + L::kOStride * t;
+      const uint64_t dq = smem_desc_kmajor(smem_u32(sQ + t * L::kTile), 128), dk0 = smem_desc_kmajor(smem_u32(sKV), 128), dv0 = desc_mnmajor(smem_u32(sKV), kPanel);
+      int g = 0, items = 0, uses = 0;               // key tiles of the CTA; items and key tiles of this query tile
       bool ok = true;
-      auto scores = [&](const Pos& p, int t) {
-        const int slot = 2 * p.g, st = slot % kStages;
-        if (t == 0 && !(ok = wait(&sh->full[st], (slot / kStages) & 1, sh, a, 10))) return;
-        if (p.j == 0) {
-          if (!(ok = wait(&sh->q_full[t], nq[t] & 1, sh, a, 11))) return;
-          ++nq[t];
-        }
+      // The two warps take turns: [P_0 V, next S_0], [P_1 V, next S_1], ...  Left alone their products mix, both tiles' scores are
+      // complete at the same time, both softmax groups want the special-function unit at once and the tensor cores wait for them.
+      int turns = 0;
+      auto my_turn = [&] { return ok = t == 0 && turns == 0 ? true : wait(&sh->turn[t], (t == 0 ? turns - 1 : turns) & 1, sh, a, 16); };
+      auto pass = [&] { mbar_arrive(&sh->turn[t ^ 1]); };
+      auto scores = [&](bool first, bool last_of_item, bool alone) {
+        const int slot = 2 * g, st = slot % kStages;
+        if (!(ok = wait(&sh->full[st], (slot / kStages) & 1, sh, a, 10))) return;
+        if (first && !(ok = wait(&sh->q_full[t], items & 1, sh, a, 11))) return;
+        // (no fence: what these columns held was read in front of the hand-over that the product issued last has waited for)
         if (elect_one()) {
-          tc_fence_after();
-          const uint64_t dq = smem_desc_kmajor(smem_u32(sQ + t * L::kTile), 128), dk = smem_desc_kmajor(smem_u32(sKV + st * L::kTile), 128);
+          const uint64_t dk = dk0 + st * (L::kTile >> 4);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint32_t at = (k / 4) * (kPanel >> 4) + 2 * (k % 4);
-            mma_f16_ss(tmem + 128 * t, dq + at, dk + at, idesc_s, k > 0);
+            mma_f16_ss(s_at, dq + at, dk + at, idesc_s, k > 0);
           }
           mma_commit(&sh->s_full[t]);
-          if (p.j == p.w.nt - 1) mma_commit(&sh->q_free[t]);
-          if (t == (p.w.two ? 1 : 0)) mma_commit(&sh->empty[st]);
+          pass();
+          if (last_of_item) mma_commit(&sh->q_free[t]);
+          mma_commit(&sh->empty[st]);
+          if (alone) mma_commit(&sh->empty[st]);    // for the query tile that is not there
         }
         __syncwarp();
       };
-      auto outputs = [&](const Pos& p, int t) {
-        const int slot = 2 * p.g + 1, st = slot % kStages;
-        if (t == 0) {
-          if (!(ok = wait(&sh->full[st], (slot / kStages) & 1, sh, a, 12))) return;
-          if (masked && !(ok = wait(&sh->fixed[p.g & 1], (p.g >> 1) & 1, sh, a, 13))) return;
-        }
-        if (p.j == 0) {
-          if (!(ok = wait(&sh->o_free[t], (no[t] & 1) ^ 1, sh, a, 14))) return;
-          ++no[t];
-        }
-        if (!(ok = wait(&sh->p_full[t], np[t] & 1, sh, a, 15))) return;
-        ++np[t];
+      auto outputs = [&](bool first, bool last_of_item, bool alone) {
+        const int slot = 2 * g + 1, st = slot % kStages;
+        if (!(ok = wait(&sh->full[st], (slot / kStages) & 1, sh, a, 12))) return;
+        if (masked && !(ok = wait(&sh->fixed[g & 1], (g >> 1) & 1, sh, a, 13))) return;
+        if (first && !(ok = wait(&sh->o_free[t], (items & 1) ^ 1, sh, a, 14))) return;
+        if (!(ok = wait(&sh->p_full[t], uses & 1, sh, a, 15))) return;
+        if (!my_turn()) return;
+        ++turns;
         if (elect_one()) {
           tc_fence_after();
-          const uint64_t dv = desc_mnmajor(smem_u32(sKV + st * L::kTile), kPanel);
+          const uint64_t dv = dv0 + st * (L::kTile >> 4);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) mma_f16_ts(tmem + L::kO + L::kOStride * t, tmem + 128 * t + 8 * k, dv + 128 * k, idesc_o, (p.j > 0) | (k > 0));
-          if (p.j == p.w.nt - 1) mma_commit(&sh->o_full[t]);
-          if (t == (p.w.two ? 1 : 0)) mma_commit(&sh->empty[st]);
+          for (int k = 0; k < 8; ++k) mma_f16_ts(o_at, s_at + 8 * k, dv + 128 * k, idesc_o, !first | (k > 0));
+          if (last_of_item) mma_commit(&sh->o_full[t]);
+          mma_commit(&sh->empty[st]);
+          if (alone) mma_commit(&sh->empty[st]);
         }
         __syncwarp();
       };
-      bool more = next(cur);
-      if (more) {
-        scores(cur, 0);
-        if (ok && cur.w.two) scores(cur, 1);
+      // S(0), [P(0) V, S(1)], [P(1) V, S(2)], ... across items.  A turn for every key tile, also where this query tile is not there.
+      Item w, x;
+      auto next_item = [&](int from, Item& it) {    // the next item that has keys
+        for (; from < a.items; from += gridDim.x) {
+          it = item_of(a, from);
+          if (it.nt > 0) break;
+        }
+        return from;
+      };
+      auto here = [&](const Item& it) { return t == 0 || it.two; };
+      int idx = next_item(blockIdx.x, w);
+      if (idx < a.items) {
+        if (!my_turn()) {
+        } else if (++turns, here(w)) {
+          scores(true, w.nt == 1, !w.two);
+        } else if (elect_one()) {
+          pass();
+        }
       }
-      while (ok && more) {
-        Pos nx = cur;
-        const bool has = next(nx);
-        outputs(cur, 0);
-        if (ok && has) scores(nx, 0);
-        if (ok && cur.w.two) outputs(cur, 1);
-        if (ok && has && nx.w.two) scores(nx, 1);
-        cur = nx;
-        more = has;
+      while (ok && idx < a.items) {
+        const int nidx = next_item(idx + gridDim.x, x);
+        for (int j = 0; ok && j < w.nt; ++j) {
+          const bool end = j + 1 == w.nt, nx_here = end ? nidx < a.items && here(x) : here(w);
+          if (here(w)) {
+            outputs(j == 0, end, !w.two);
+            ++uses;
+            if (end) ++items;
+          } else if (my_turn()) {
+            ++turns;
+          }
+          ++g;
+          if (!ok) break;
+          if (nx_here) scores(end, end ? x.nt == 1 : j + 2 == w.nt, end ? !x.two : !w.two);
+          else if (elect_one()) pass();
+          __syncwarp();
+        }
+        w = x;
+        idx = nidx;
       }
-      if (elect_one()) mma_commit(&sh->drain);
+      if (elect_one()) mma_commit(&sh->drain[t]);
       __syncwarp();
-      mbar_wait(&sh->drain, 0, attn::kDrainLimit);
-    } else if (warp == 14 && masked) {
+      mbar_wait(&sh->drain[t], 0, attn::kDrainLimit);
+    } else if (warp == 2 && masked) {
       // -------------------------------------------------------------------------------- value rows of masked keys
       // 0 times an infinity or NaN is NaN: rows whose probability is 0 must hold numbers.
       int g = 0;
@@ -337,10 +337,10 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
       }
     }
-  } else if (warp < 8) {
-    // ---------------------------------------------------------------------------------- softmax, one query tile a warpgroup
+  } else if (warp < 12) {
     reg_inc<kRegSoftmax>();
-    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    // ---------------------------------------------------------------------------------- softmax, one query tile a warpgroup
+    const int t = (warp >> 2) - 1, row = (warp & 3) * 32 + lane;
     const uint32_t s_col = lane_base + 128 * t, o_col = lane_base + L::kO + L::kOStride * t;
     int g = 0, uses = 0, items = 0;
     bool ok = true;
@@ -422,8 +422,8 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       ++items;
     }
   } else {
-    // ---------------------------------------------------------------------------------- epilogue
     reg_dec<kRegEpi>();
+    // ---------------------------------------------------------------------------------- epilogue
     using Out = attn::OutTile<64>;                  // rows leave in lines of 128 bytes
     const int quarter = warp & 3;
     const uint32_t tile = smem_u32(sOut) + quarter * 32 * Out::ROW;
@@ -435,62 +435,63 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       for (int t = 0; t < (w.two ? 2 : 1); ++t) {
         const int row0 = (w.q0 + t) * 128 + quarter * 32, rows = min(32, a.Nq - row0);
         float inv = 0.f, lse2 = -INFINITY;
-        uint32_t out[D / 2];
         // my row of the outputs' [B * H][N_q], behind those of the splits in front of this one
         const int64_t line = ((int64_t)w.split * a.heads + w.b * a.H + w.h) * a.Nq + row0 + lane;
-        float* po = a.part_o + line * D;
         if (w.nt > 0) {
           if (!(ok = wait(&sh->o_full[t], uses[t] & 1, sh, a, 40))) break;
           const float2 ml = sh->ml[uses[t] & 1][t][quarter * 32 + lane];
+          const float l = ml.y;
           ++uses[t];
-          inv = ml.y > 0.f || ml.y != ml.y ? 1.0f / ml.y : 0.f;       // (a sum of NaN makes a row of NaN)
-          lse2 = ml.y == 0.f ? -INFINITY : ml.x + log2f(ml.y);
+          inv = l > 0.f || l != l ? 1.0f / l : 0.f;                   // (a sum of NaN makes a row of NaN)
+          lse2 = l == 0.f ? -INFINITY : ml.x + log2f(l);
           tc_fence_after();
-          const uint32_t o_col = lane_base + L::kO + L::kOStride * t;
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t r[32];
+        }
+        const uint32_t o_col = lane_base + L::kO + L::kOStride * t;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {                            // 32 channels
+          uint32_t r[32];
+          if (w.nt > 0) {
             tmem_ld32(o_col + 32 * c, r);
             tmem_wait_ld();
-            if (a.splits > 1) {
-              if (lane < rows)
+            if (c == D / 32 - 1) {
+              tc_fence_before();
+              mbar_arrive(&sh->o_free[t]);
+            }
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                  reinterpret_cast<float4*>(po)[8 * c + i] = make_float4(__uint_as_float(r[4 * i]) * inv, __uint_as_float(r[4 * i + 1]) * inv,
-                                                                         __uint_as_float(r[4 * i + 2]) * inv, __uint_as_float(r[4 * i + 3]) * inv);
-            } else {
+            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * inv);
+          } else {
 #pragma unroll
-              for (int i = 0; i < 16; ++i) out[16 * c + i] = pack16<T>(__uint_as_float(r[2 * i]) * inv, __uint_as_float(r[2 * i + 1]) * inv);
+            for (int i = 0; i < 32; ++i) r[i] = 0;
+          }
+          if (a.splits > 1) {
+            float4* po = reinterpret_cast<float4*>(a.part_o + line * D + 32 * c);
+            if (lane < rows)
+#pragma unroll
+              for (int i = 0; i < 32; i += 4)
+                po[i / 4] = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+            continue;
+          }
+          if ((c & 1) == 0) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");        // the copy in front has read the rows
+            __syncwarp();
+          }
+          auto two = [&](int i) { return pack16<T>(__uint_as_float(r[i]), __uint_as_float(r[i + 1])); };
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sts128(Out::chunk(tile, lane, 4 * (c & 1) + i), two(8 * i), two(8 * i + 2), two(8 * i + 4), two(8 * i + 6));
+          if (c & 1) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && rows > 0) {               // (rows behind the last query are left as they are)
+              asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(reinterpret_cast<uint64_t>(&tm_o)),
+                           "r"(tile), "r"(32 * c - 32), "r"(row0), "r"(w.h), "r"(w.b)
+                           : "memory");
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
           }
-          tc_fence_before();
-          mbar_arrive(&sh->o_free[t]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < D / 2; ++i) out[i] = 0;
-          if (a.splits > 1 && lane < rows)
-#pragma unroll 1
-            for (int i = 0; i < D / 4; ++i) reinterpret_cast<float4*>(po)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        if (a.splits > 1) {
-          if (lane < rows) a.part_lse[line] = lse2;
-          continue;
-        }
-        if (a.lse && lane < rows) a.lse[line] = lse2 * kLn2;
-#pragma unroll
-        for (int half = 0; half < D / 64; ++half) {
-          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");          // the copy in front has read the rows
-          __syncwarp();
-#pragma unroll
-          for (int c = 0; c < 8; ++c) sts128(Out::chunk(tile, lane, c), out[32 * half + 4 * c], out[32 * half + 4 * c + 1], out[32 * half + 4 * c + 2], out[32 * half + 4 * c + 3]);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0 && rows > 0) {                 // (rows behind the last query are left as they are)
-            asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(reinterpret_cast<uint64_t>(&tm_o)), "r"(tile),
-                         "r"(64 * half), "r"(row0), "r"(w.h), "r"(w.b)
-                         : "memory");
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          }
+        if (lane < rows) {
+          if (a.splits > 1) a.part_lse[line] = lse2;
+          else if (a.lse) a.lse[line] = lse2 * kLn2;
         }
       }
     }
@@ -498,7 +499,7 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 14) tmem_dealloc<512>(tmem);
+  if (warp == 2) tmem_dealloc<512>(tmem);
 }
 
 // Joins the parts of a row: o = sum w_s o_s / sum w_s, w_s = 2^(lse_s - max lse), in the order of the splits.  A warp a row.
