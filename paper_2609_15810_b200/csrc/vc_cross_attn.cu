@@ -64,6 +64,7 @@ struct Smem {
 struct Item {
   int b, h, q0, split, t0, nt, len;
   bool two;
+  __device__ __forceinline__ bool has(int t, bool halves) const { return halves ? nt > t : t == 0 || two; }      // query tile t (half t of the keys)
 };
 
 __device__ __forceinline__ Item item_of(const CrossArgs& a, int idx) {
@@ -121,7 +122,8 @@ template <int D> struct Lay {
   static constexpr uint32_t kO = 256, kOStride = D;
 };
 
-template <typename T, int D>
+// HALVES: one query tile an item; its even and its odd key tiles take the places of two query tiles, and the epilogue joins them.
+template <typename T, int D, bool HALVES>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ CrossArgs a) {
@@ -195,12 +197,12 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           __syncwarp();
           fill(&tm_k, row, hk * a.k_h, w.b * a.k_b);
           if (j == 0) {                             // queries, each tile's when its predecessor's last scores are complete
-            for (int t = 0; t < (w.two ? 2 : 1); ++t) {
+            for (int t = 0; t < 2 && w.has(t, HALVES); ++t) {
               if (!(ok = wait(&sh->q_free[t], (n[t] & 1) ^ 1, sh, a, 3))) break;
               if (elect_one()) {
                 mbar_expect_tx(&sh->q_full[t], L::kTile);
                 for (int c = 0; c < D / 64; ++c)
-                  tma_load_4d(sQ + t * L::kTile + c * kPanel, &tm_q, &sh->q_full[t], 64 * c, (w.q0 + t) * 128, w.h * a.q_h, w.b * a.q_b);
+                  tma_load_4d(sQ + t * L::kTile + c * kPanel, &tm_q, &sh->q_full[t], 64 * c, (HALVES ? w.q0 : w.q0 + t) * 128, w.h * a.q_h, w.b * a.q_b);
               }
               __syncwarp();
               ++n[t];
@@ -227,8 +229,8 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       // The two warps take turns: [P_0 V, next S_0], [P_1 V, next S_1], ...  Left alone their products mix, both tiles' scores are
       // complete at the same time, both softmax groups want the special-function unit at once and the tensor cores wait for them.
       int turns = 0;
-      auto my_turn = [&] { return ok = t == 0 && turns == 0 ? true : wait(&sh->turn[t], (t == 0 ? turns - 1 : turns) & 1, sh, a, 16); };
-      auto pass = [&] { mbar_arrive(&sh->turn[t ^ 1]); };
+      auto my_turn = [&] { return ok = HALVES || t == 0 && turns == 0 ? true : wait(&sh->turn[t], (t == 0 ? turns - 1 : turns) & 1, sh, a, 16); };
+      auto pass = [&] { if (!HALVES) mbar_arrive(&sh->turn[t ^ 1]); };
       auto scores = [&](bool first, bool last_of_item, bool alone) {
         const int slot = 2 * g, st = slot % kStages;
         if (!(ok = wait(&sh->full[st], (slot / kStages) & 1, sh, a, 10))) return;
@@ -268,7 +270,6 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         __syncwarp();
       };
-      // S(0), [P(0) V, S(1)], [P(1) V, S(2)], ... across items.  A turn for every key tile, also where this query tile is not there.
       Item w, x;
       auto next_item = [&](int from, Item& it) {    // the next item that has keys
         for (; from < a.items; from += gridDim.x) {
@@ -277,35 +278,63 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         return from;
       };
-      auto here = [&](const Item& it) { return t == 0 || it.two; };
       int idx = next_item(blockIdx.x, w);
-      if (idx < a.items) {
-        if (!my_turn()) {
-        } else if (++turns, here(w)) {
-          scores(true, w.nt == 1, !w.two);
-        } else if (elect_one()) {
-          pass();
-        }
-      }
-      while (ok && idx < a.items) {
-        const int nidx = next_item(idx + gridDim.x, x);
-        for (int j = 0; ok && j < w.nt; ++j) {
-          const bool end = j + 1 == w.nt, nx_here = end ? nidx < a.items && here(x) : here(w);
-          if (here(w)) {
-            outputs(j == 0, end, !w.two);
-            ++uses;
-            if (end) ++items;
-          } else if (my_turn()) {
-            ++turns;
-          }
-          ++g;
+      if constexpr (HALVES) {
+        // My key tiles one by one, and no turns: a tile's keys and values have one reader.
+        g = t;
+        auto skip = [&] {                           // items that have none for me
+          for (; idx < a.items && w.nt <= t; idx = next_item(idx + gridDim.x, w)) g += w.nt;
+        };
+        skip();
+        if (idx < a.items) scores(true, w.nt <= t + 2, true);
+        for (int j = t; ok && idx < a.items;) {
+          const bool end = j + 2 >= w.nt;
+          outputs(j == t, end, true);
+          ++uses;
           if (!ok) break;
-          if (nx_here) scores(end, end ? x.nt == 1 : j + 2 == w.nt, end ? !x.two : !w.two);
-          else if (elect_one()) pass();
-          __syncwarp();
+          if (end) {
+            ++items;
+            g += w.nt - j + t;
+            idx = next_item(idx + gridDim.x, w);
+            skip();
+            j = t;
+          } else {
+            g += 2;
+            j += 2;
+          }
+          if (idx < a.items) scores(j == t, j + 2 >= w.nt, true);
         }
-        w = x;
-        idx = nidx;
+      } else {
+        // S(0), [P(0) V, S(1)], [P(1) V, S(2)], ... across items.  A turn for every key tile, also where this query tile is not there.
+        auto here = [&](const Item& it) { return t == 0 || it.two; };
+        if (idx < a.items) {
+          if (!my_turn()) {
+          } else if (++turns, here(w)) {
+            scores(true, w.nt == 1, !w.two);
+          } else if (elect_one()) {
+            pass();
+          }
+        }
+        while (ok && idx < a.items) {
+          const int nidx = next_item(idx + gridDim.x, x);
+          for (int j = 0; ok && j < w.nt; ++j) {
+            const bool end = j + 1 == w.nt, nx_here = end ? nidx < a.items && here(x) : here(w);
+            if (here(w)) {
+              outputs(j == 0, end, !w.two);
+              ++uses;
+              if (end) ++items;
+            } else if (my_turn()) {
+              ++turns;
+            }
+            ++g;
+            if (!ok) break;
+            if (nx_here) scores(end, end ? x.nt == 1 : j + 2 == w.nt, end ? !x.two : !w.two);
+            else if (elect_one()) pass();
+            __syncwarp();
+          }
+          w = x;
+          idx = nidx;
+        }
       }
       if (elect_one()) mma_commit(&sh->drain[t]);
       __syncwarp();
@@ -347,9 +376,10 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
       const Item w = item_of(a, idx);
       if (w.nt == 0) continue;
-      if (t && !w.two) { g += w.nt; continue; }
+      if (!w.has(t, HALVES)) { g += w.nt; continue; }
       float m = -INFINITY, l = 0.f;                 // reference (log2 domain) and row sum
-      for (int j = 0; j < w.nt; ++j, ++g) {
+      const int step = HALVES ? 2 : 1, j0 = HALVES ? t : 0;
+      for (int j = j0; j < w.nt; j += step) {
         if (!(ok = wait(&sh->s_full[t], uses & 1, sh, a, 30))) break;
         ++uses;
         tc_fence_after();
@@ -357,7 +387,7 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         tmem_ld32(s_col, s0); tmem_ld32(s_col + 32, s1); tmem_ld32(s_col + 64, s2); tmem_ld32(s_col + 96, s3);
         tmem_wait_ld();
         if (w.len - (w.t0 + j) * 128 < 128 || a.key_mask) {
-          const uint4 kept = *reinterpret_cast<const uint4*>(sh->bits[g & 3]);
+          const uint4 kept = *reinterpret_cast<const uint4*>(sh->bits[(g + j) & 3]);
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             if (!(kept.x >> i & 1)) s0[i] = 0xff800000u;
@@ -375,7 +405,7 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           mx[3] = max3(mx[3], __uint_as_float(s3[i]), __uint_as_float(s3[i + 1]));
         }
         const float top = a.sl * max3(max3(mx[0], __uint_as_float(s0[31]), mx[1]), max3(__uint_as_float(s1[31]), mx[2], __uint_as_float(s2[31])), fmaxf(mx[3], __uint_as_float(s3[31])));
-        if (j == 0) {
+        if (j == j0) {
           m = top;
         } else if (__any_sync(0xffffffffu, top > m + kRescale)) {
           const float m_new = fmaxf(m, top), alpha = m == m_new ? 1.f : ex2_approx(m - m_new);
@@ -414,11 +444,12 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         l += a0 + a1;
         // In front of the last hand-over: the product behind it, when complete, says that these are there too.  Two slots do: the
         // tile's next item but one gets here only when the next one's first product has seen the epilogue of this one.
-        if (j == w.nt - 1) sh->ml[items & 1][t][row] = make_float2(m, l);
+        if (j + step >= w.nt) sh->ml[items & 1][t][row] = make_float2(m, l);
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sh->p_full[t]);
       }
+      g += w.nt;
       ++items;
     }
   } else {
@@ -432,18 +463,29 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
       const Item w = item_of(a, idx);
 #pragma unroll 1
-      for (int t = 0; t < (w.two ? 2 : 1); ++t) {
+      for (int t = 0; t < (w.two ? 2 : 1); ++t) {       // (the halves of the keys are joined in one pass)
         const int row0 = (w.q0 + t) * 128 + quarter * 32, rows = min(32, a.Nq - row0);
-        float inv = 0.f, lse2 = -INFINITY;
+        const bool both = HALVES && w.nt > 1;
+        float inv = 0.f, inv1 = 0.f, lse2 = -INFINITY;
         // my row of the outputs' [B * H][N_q], behind those of the splits in front of this one
         const int64_t line = ((int64_t)w.split * a.heads + w.b * a.H + w.h) * a.Nq + row0 + lane;
         if (w.nt > 0) {
-          if (!(ok = wait(&sh->o_full[t], uses[t] & 1, sh, a, 40))) break;
-          const float2 ml = sh->ml[uses[t] & 1][t][quarter * 32 + lane];
-          const float l = ml.y;
+          if (!(ok = wait(&sh->o_full[t], uses[t] & 1, sh, a, 40)) || (both && !(ok = wait(&sh->o_full[1], uses[1] & 1, sh, a, 41)))) break;
+          float2 ml = sh->ml[uses[t] & 1][t][quarter * 32 + lane];
           ++uses[t];
-          inv = l > 0.f || l != l ? 1.0f / l : 0.f;                   // (a sum of NaN makes a row of NaN)
-          lse2 = l == 0.f ? -INFINITY : ml.x + log2f(l);
+          float f0 = 1.f, f1 = 0.f;
+          if (both) {                                 // o = (2^(m0 - m) O_0 + 2^(m1 - m) O_1) / (2^(m0 - m) l0 + 2^(m1 - m) l1)
+            const float2 ml1 = sh->ml[uses[1] & 1][1][quarter * 32 + lane];
+            ++uses[1];
+            const float m = fmaxf(ml.x, ml1.x), ms = m == -INFINITY ? 0.f : m;
+            f0 = ex2_approx(ml.x - ms);
+            f1 = ex2_approx(ml1.x - ms);
+            ml = make_float2(m, f0 * ml.y + f1 * ml1.y);
+          }
+          const float total = ml.y > 0.f || ml.y != ml.y ? 1.0f / ml.y : 0.f;     // (a sum of NaN makes a row of NaN)
+          inv = f0 * total;
+          inv1 = f1 * total;
+          lse2 = ml.y == 0.f ? -INFINITY : ml.x + log2f(ml.y);
           tc_fence_after();
         }
         const uint32_t o_col = lane_base + L::kO + L::kOStride * t;
@@ -453,12 +495,23 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           if (w.nt > 0) {
             tmem_ld32(o_col + 32 * c, r);
             tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * inv);
+            if (both) {
+#pragma unroll
+              for (int q = 0; q < 2; ++q) {
+                uint32_t r1[16];
+                tmem_ld16(o_col + L::kOStride + 32 * c + 16 * q, r1);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) r[16 * q + i] = __float_as_uint(fmaf(__uint_as_float(r1[i]), inv1, __uint_as_float(r[16 * q + i])));
+              }
+            }
             if (c == D / 32 - 1) {
               tc_fence_before();
               mbar_arrive(&sh->o_free[t]);
+              if (both) mbar_arrive(&sh->o_free[1]);
             }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * inv);
           } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) r[i] = 0;
@@ -595,7 +648,7 @@ bool make_map16(CUtensorMap* m, const void* base, const vc_strides& s, int B, in
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool HALVES>
 cudaError_t launch_cross(const vc_cross_params& r, const Plan& pl, CrossArgs& a, const void* q, const void* k, const void* v, cudaStream_t s) {
   alignas(64) CUtensorMap tq, tk, tv, to;
   const bool any = r.N_kv > 0;                      // without keys nothing is loaded, and any valid map will do
@@ -604,10 +657,10 @@ cudaError_t launch_cross(const vc_cross_params& r, const Plan& pl, CrossArgs& a,
   tk = tv = tq;
   if (any && (!make_map16(&tk, k, r.k, r.B, r.H_kv, r.N_kv, D, 128, &a.k_b, &a.k_h) || !make_map16(&tv, v, r.v, r.B, r.H_kv, r.N_kv, D, 128, &a.v_b, &a.v_h)))
     return cudaErrorUnknown;
-  cudaError_t e = allow_smem<cross_attn_kernel<T, D>>();
+  cudaError_t e = allow_smem<cross_attn_kernel<T, D, HALVES>>();
   if (e != cudaSuccess) return e;
   const int grid = pl.items < sm_count() ? (int)pl.items : sm_count();
-  e = launch_overlapped(cross_attn_kernel<T, D>, dim3((unsigned)grid), kThreads, Lay<D>::kSmem, s, tq, tk, tv, to, a);
+  e = launch_overlapped(cross_attn_kernel<T, D, HALVES>, dim3((unsigned)grid), kThreads, Lay<D>::kSmem, s, tq, tk, tv, to, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
   if (pl.splits > 1) {
@@ -616,6 +669,11 @@ cudaError_t launch_cross(const vc_cross_params& r, const Plan& pl, CrossArgs& a,
     count_launches(1);
   }
   return cudaSuccess;
+}
+
+template <typename T, int D>
+cudaError_t launch_halves(const vc_cross_params& r, const Plan& pl, CrossArgs& a, const void* q, const void* k, const void* v, cudaStream_t s) {
+  return pl.tiles_per_item == 1 ? launch_cross<T, D, true>(r, pl, a, q, k, v, s) : launch_cross<T, D, false>(r, pl, a, q, k, v, s);
 }
 
 }  // namespace
@@ -652,7 +710,7 @@ extern "C" vc_status vc_cross_attn(const vc_cross_params* p, const void* q, cons
   a.nonblocking = attn::attn_wait_nonblocking();
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e;
-  if (r.dtype == VC_DTYPE_BF16) e = r.d == 128 ? launch_cross<__nv_bfloat16, 128>(r, pl, a, q, k, v, s) : launch_cross<__nv_bfloat16, 64>(r, pl, a, q, k, v, s);
-  else e = r.d == 128 ? launch_cross<__half, 128>(r, pl, a, q, k, v, s) : launch_cross<__half, 64>(r, pl, a, q, k, v, s);
+  if (r.dtype == VC_DTYPE_BF16) e = r.d == 128 ? launch_halves<__nv_bfloat16, 128>(r, pl, a, q, k, v, s) : launch_halves<__nv_bfloat16, 64>(r, pl, a, q, k, v, s);
+  else e = r.d == 128 ? launch_halves<__half, 128>(r, pl, a, q, k, v, s) : launch_halves<__half, 64>(r, pl, a, q, k, v, s);
   return e == cudaSuccess ? VC_OK : VC_ERR_CUDA;
 }
