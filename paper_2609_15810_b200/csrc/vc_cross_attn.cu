@@ -155,6 +155,7 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   pdl_wait();
   if (warp == 2) { tmem_alloc<512>(&sh->tmem_base); tmem_relinquish(); }
   if (tid == 0 && blockIdx.x == 0) *a.status = 0;
+  if (a.splits > 1) pdl_allow();               // (what follows then is the launch that joins the parts: it may stand by)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

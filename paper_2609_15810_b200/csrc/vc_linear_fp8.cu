@@ -97,6 +97,30 @@ template <> __device__ __forceinline__ uint4 pack_chunk<__nv_bfloat16>(const flo
 template <> __device__ __forceinline__ uint4 pack_chunk<__half>(const float* f) {
   return make_uint4(pack16<__half>(f[0], f[1]), pack16<__half>(f[2], f[3]), pack16<__half>(f[4], f[5]), pack16<__half>(f[6], f[7]));
 }
+// The same as one copy of the warp's 32 rows at a time, where rows of `out` start on 16-byte boundaries; what lies outside of it the copy leaves out.
+template <typename O, int COLS>
+__device__ __forceinline__ void emit_copies(const float (&y)[COLS], uint32_t tile, const CUtensorMap* map, int col0, int row0, int rows, int lane) {
+  using Out = attn::OutTile<64>;
+  constexpr int kPer = 16 / sizeof(O), kPass = 8 * kPer;
+#pragma unroll
+  for (int p = 0; p < COLS / kPass; ++p) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");        // the copy in front has read the tile
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint4 v = pack_chunk<O>(y + p * kPass + c * kPer);
+      sts128(Out::chunk(tile, lane, c), v.x, v.y, v.z, v.w);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0 && rows > 0) {
+      asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(tile),
+                   "r"(col0 + p * kPass), "r"(row0)
+                   : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+}
 template <typename O, int COLS>
 __device__ __forceinline__ void emit_rows(const float (&y)[COLS], uint32_t tile, O* dst, int64_t ld, int rows, int cols, bool vec, int lane) {
   using Out = attn::OutTile<64>;                               // (128 bytes a row, whatever the type)
@@ -131,7 +155,8 @@ __device__ __forceinline__ void emit_rows(const float (&y)[COLS], uint32_t tile,
 
 template <bool SWAP, int TN>
 __global__ void __launch_bounds__(kThreads, 1)
-linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ LinearArgs a) {
+linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+                  const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ LinearArgs a) {
   using C = Cfg<SWAP, TN>;
   using S = Smem<C::kStages, C::kBufs>;
   constexpr int kRegAdd = 216, kRegCtl = 72;
@@ -152,6 +177,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
   pdl_wait();
   if (warp == 10) { tmem_alloc<C::kTmem>(&sh->tmem_base); tmem_relinquish(); }
   if (tid == 0 && blockIdx.x == 0) *a.status = 0;
+  if (a.splits > 1) pdl_allow();               // (what follows then is the launch that joins the parts: it may stand by)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -210,33 +236,46 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     constexpr int kCols = C::kCols, kChunk = kCols < 32 ? kCols : 32, kChunks = kCols / kChunk;
     const int group = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + group * kCols;
+    constexpr int kBias = SWAP ? 1 : (kCols + 31) / 32;
+    const bool whole = a.splits == 1;
+    // An item's scales (of one block of K) and biases, fetched ahead: while the block in front is added, or the item in front written.
+    // xa: of my row, or (SWAP) of row `lane` of my columns, xb of row 32 + lane; bias: of my columns lane, 32 + lane, ..., or (SWAP) of my row.
+    float xa = 0.f, xb = 0.f, wv = 0.f, bias[kBias] = {};
+    auto fetch = [&](const Item& w, int kb) {
+      const float* xp = a.xs + (int64_t)kb * a.M;
+      if constexpr (SWAP) {
+        const int m = w.b0 + lane;
+        xa = lane < kCols && m < a.M ? __ldg(xp + m) : 0.f;
+        if constexpr (kCols > 32) xb = m + 32 < a.M ? __ldg(xp + m + 32) : 0.f;
+      } else {
+        xa = w.a0 + row < a.M ? __ldg(xp + w.a0 + row) : 0.f;
+      }
+      const int n0 = SWAP ? w.a0 : w.b0 + group * kCols;       // my (first) weight row; all of mine lie in its block of 128
+      wv = __ldg(a.ws + (int64_t)min(n0 >> 7, (a.N - 1) >> 7) * a.blocks + kb);
+    };
+    auto fetch_item = [&](const Item& w) {
+      fetch(w, w.kb0);
+      if (whole && a.bias) {
+#pragma unroll
+        for (int i = 0; i < kBias; ++i) {
+          const int col = SWAP ? w.a0 + row : w.b0 + group * kCols + 32 * i + lane;
+          bias[i] = col < a.N ? load1(a.bias, a.bias_dtype, col) : 0.f;
+        }
+      }
+    };
     int n = 0;
     bool ok = true;
+    Item w = item_of<TN>(a, blockIdx.x);
+    fetch_item(w);
     for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
-      const Item w = item_of<TN>(a, idx);
       uint64_t acc[kCols / 2];
 #pragma unroll
       for (int i = 0; i < kCols / 2; ++i) acc[i] = 0;
-      const int m0 = SWAP ? w.b0 : w.a0 + row;                 // my row of x (SWAP: my columns' first)
-      const int n0 = SWAP ? w.a0 : w.b0 + group * kCols;       // my (first) weight row; all my weight rows lie in its block of 128
-      const float* wsp = a.ws + (int64_t)min(n0 >> 7, (a.N - 1) >> 7) * a.blocks;
-      // Scales of a block, fetched one block ahead: that of my row, or (SWAP) of row `lane` and 32 + lane of my columns.
-      float xa = 0.f, xb = 0.f, wv = 0.f;
-      auto fetch = [&](int kb) {
-        const float* xp = a.xs + (int64_t)kb * a.M;
-        if constexpr (SWAP) {
-          xa = m0 + lane < a.M ? __ldg(xp + m0 + lane) : 0.f;
-          if constexpr (kCols > 32) xb = m0 + 32 + lane < a.M ? __ldg(xp + m0 + 32 + lane) : 0.f;
-        } else {
-          xa = m0 < a.M ? __ldg(xp + m0) : 0.f;
-        }
-        wv = __ldg(wsp + kb);
-      };
-      fetch(w.kb0);
+      const int m0 = SWAP ? w.b0 : w.a0 + row, n0 = SWAP ? w.a0 : w.b0 + group * kCols;
       for (int kb = w.kb0; kb < w.kb1; ++kb, ++n) {
         const int buf = n % C::kBufs;
         const float fa = xa * wv, fb = xb * wv;
-        if (kb + 1 < w.kb1) fetch(kb + 1);
+        if (kb + 1 < w.kb1) fetch(w, kb + 1);
         if (!(ok = wait(&sh->acc_full[buf], (n / C::kBufs) & 1, sh, a, 20))) break;
         tc_fence_after();
         const uint32_t at = lane_base + buf * TN;
@@ -272,44 +311,47 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
       float y[kCols];
 #pragma unroll
       for (int i = 0; i < kCols / 2; ++i) unpack2(acc[i], y[2 * i], y[2 * i + 1]);
-      const bool whole = a.splits == 1;
+      float mine[kBias];
+#pragma unroll
+      for (int i = 0; i < kBias; ++i) mine[i] = bias[i];
+      const Item now = w;
+      if (idx + (int)gridDim.x < a.items) {
+        w = item_of<TN>(a, idx + gridDim.x);
+        fetch_item(w);
+      }
       if constexpr (SWAP) {
-        const int col = w.a0 + row;
+        const int col = now.a0 + row;
         if (col < a.N) {
-          const float bias = whole && a.bias ? load1(a.bias, a.bias_dtype, col) : 0.f;
 #pragma unroll
           for (int i = 0; i < kCols; ++i) {
             if (m0 + i >= a.M) break;
-            if (!whole) a.part[((int64_t)w.split * a.M + m0 + i) * a.ldp + col] = y[i];
-            else if (a.out_dtype == VC_DTYPE_BF16) static_cast<__nv_bfloat16*>(a.out)[(m0 + i) * a.ldo + col] = __float2bfloat16_rn(y[i] + bias);
-            else if (a.out_dtype == VC_DTYPE_FP16) static_cast<__half*>(a.out)[(m0 + i) * a.ldo + col] = __float2half_rn(y[i] + bias);
-            else static_cast<float*>(a.out)[(m0 + i) * a.ldo + col] = y[i] + bias;
+            const float v = y[i] + mine[0];
+            if (!whole) a.part[((int64_t)now.split * a.M + m0 + i) * a.ldp + col] = v;
+            else if (a.out_dtype == VC_DTYPE_BF16) static_cast<__nv_bfloat16*>(a.out)[(m0 + i) * a.ldo + col] = __float2bfloat16_rn(v);
+            else if (a.out_dtype == VC_DTYPE_FP16) static_cast<__half*>(a.out)[(m0 + i) * a.ldo + col] = __float2half_rn(v);
+            else static_cast<float*>(a.out)[(m0 + i) * a.ldo + col] = v;
           }
         }
       } else {
-        const int row0 = w.a0 + (warp & 3) * 32, rows = min(32, a.M - row0), cols = min(kCols, a.N - n0);
+        const int row0 = now.a0 + (warp & 3) * 32, rows = min(32, a.M - row0), cols = min(kCols, a.N - n0);
         const uint32_t tile = smem_u32(sOut) + warp * 4096;
         if (whole && a.bias) {
 #pragma unroll
-          for (int i = 0; i < kCols; i += 8) {
-            if (i + 8 <= cols) {
-              float b8[8];
-              load8(a.bias, a.bias_dtype, n0 + i, b8);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) y[i + e] += b8[e];
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (i + e < cols) y[i + e] += load1(a.bias, a.bias_dtype, n0 + i + e);
-            }
-          }
+          for (int i = 0; i < kCols; ++i) y[i] += __shfl_sync(0xffffffffu, mine[i / 32], i % 32);
         }
-        if (!whole) emit_rows<float, kCols>(y, tile, a.part + ((int64_t)w.split * a.M + row0) * a.ldp + n0, a.ldp, rows, cols, true, lane);
-        else if (a.out_dtype == VC_DTYPE_BF16) emit_rows<__nv_bfloat16, kCols>(y, tile, static_cast<__nv_bfloat16*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
-        else if (a.out_dtype == VC_DTYPE_FP16) emit_rows<__half, kCols>(y, tile, static_cast<__half*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
-        else emit_rows<float, kCols>(y, tile, static_cast<float*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
+        if (whole && a.vec) {
+          if (a.out_dtype == VC_DTYPE_BF16) emit_copies<__nv_bfloat16, kCols>(y, tile, &tm_o, n0, row0, cols > 0 ? rows : 0, lane);
+          else if (a.out_dtype == VC_DTYPE_FP16) emit_copies<__half, kCols>(y, tile, &tm_o, n0, row0, cols > 0 ? rows : 0, lane);
+          else emit_copies<float, kCols>(y, tile, &tm_o, n0, row0, cols > 0 ? rows : 0, lane);
+          continue;
+        }
+        if (!whole) emit_rows<float, kCols>(y, tile, a.part + ((int64_t)now.split * a.M + row0) * a.ldp + n0, a.ldp, rows, cols, true, lane);
+        else if (a.out_dtype == VC_DTYPE_BF16) emit_rows<__nv_bfloat16, kCols>(y, tile, static_cast<__nv_bfloat16*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, false, lane);
+        else if (a.out_dtype == VC_DTYPE_FP16) emit_rows<__half, kCols>(y, tile, static_cast<__half*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, false, lane);
+        else emit_rows<float, kCols>(y, tile, static_cast<float*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, false, lane);
       }
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // the rows have left before the CTA may end
   }
   tc_fence_before();
   __syncthreads();
@@ -392,18 +434,32 @@ bool make_map8(CUtensorMap* m, const void* base, int rows, int K, int64_t ld, in
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_map_out(CUtensorMap* m, void* out, const vc_linear_params& r) {
+  attn::EncodeTiledFn fn = attn::encode_fn();
+  if (!fn) return false;
+  const int es = elem_size(r.out_dtype);
+  const cuuint64_t dims[2] = {(cuuint64_t)r.N, (cuuint64_t)r.M}, strides[1] = {(cuuint64_t)r.ldo * es};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / es), 32}, step[2] = {1, 1};
+  const CUtensorMapDataType type = r.out_dtype == VC_DTYPE_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : r.out_dtype == VC_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return fn(m, type, 2, out, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool SWAP, int TN>
 cudaError_t launch_linear(const vc_linear_params& r, const Plan& pl, const LinearArgs& a, const void* x, const void* w, cudaStream_t s) {
   using C = Cfg<SWAP, TN>;
-  alignas(64) CUtensorMap ta, tb;
+  alignas(64) CUtensorMap ta, tb, to;
   if (!make_map8(&ta, SWAP ? w : x, SWAP ? r.N : r.M, r.K, SWAP ? r.ldw : r.ldx, 128) ||
       !make_map8(&tb, SWAP ? x : w, SWAP ? r.M : r.N, r.K, SWAP ? r.ldx : r.ldw, TN))
     return cudaErrorUnknown;
+  to = ta;                                   // (read where rows leave by copies alone)
+  if (!SWAP && a.vec && pl.splits == 1 && !make_map_out(&to, a.out, r)) return cudaErrorUnknown;
   cudaError_t e = allow_smem<linear_fp8_kernel<SWAP, TN>>();
   if (e != cudaSuccess) return e;
   const int grid = pl.items < sm_count() ? (int)pl.items : sm_count();
   constexpr size_t smem = C::kStages * C::kStage + C::kOut + sizeof(Smem<C::kStages, C::kBufs>);
-  e = launch_overlapped(linear_fp8_kernel<SWAP, TN>, dim3((unsigned)grid), kThreads, smem, s, ta, tb, a);
+  e = launch_overlapped(linear_fp8_kernel<SWAP, TN>, dim3((unsigned)grid), kThreads, smem, s, ta, tb, to, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
   if (pl.splits > 1) {
