@@ -1,6 +1,6 @@
 // vc_qk_norm_rope: RMS norm of queries and keys (per head, or per token over all heads) and the position rotation.
 //
-// Bound by memory: every element is read once and written once.  A thread owns eight channels of one token and
+// Bound by memory: every element is read once and written once.  A thread owns sixteen channels of one token and
 // walks over that token's heads, so the angles of a token are formed once for all its heads (a table of the CTA's tokens in
 // shared memory), loads and stores are 16 bytes, and a head's sum of squares is a shuffle within its lanes.  The norm over
 // a token keeps the thread's part of the token in registers between the sum and the rotation: one pass over memory.
@@ -14,9 +14,11 @@ namespace {
 using namespace layer;
 
 constexpr int kThreads = 256, kMaxPairs = 128;
+// Halves whose axes are multiples of 16 channels: a pair's two channels lie in whole groups of eight, and one thread owns both groups.
+constexpr int kRotaryWhole = VC_ROTARY_HALF + 1;
 
-// Heads whose channels a thread holds in registers: three CTAs an SM then fit the register file.
-__host__ __device__ constexpr int heads_held(int elem_bytes, int rotary) { return (elem_bytes == 2 ? 8 : 4) / (rotary == VC_ROTARY_HALF ? 2 : 1); }
+// Heads whose channels a thread holds in registers: two CTAs an SM then fit the register file.
+__host__ __device__ constexpr int heads_held(int elem_bytes, int rotary) { return rotary == VC_ROTARY_HALF ? (elem_bytes == 2 ? 3 : 1) : (elem_bytes == 2 ? 5 : 2); }
 
 struct QkArgs {
   const void *x[2], *w[2];
@@ -28,6 +30,8 @@ struct QkArgs {
   int turns_taken;                 // a CTA takes that many groups of tokens, one behind the other
   bool same_type;                  // weights are of the tensors' type
   bool partial;                    // some channels are not rotated
+  // The two groups of eight channels of a lane (255: none), and (kRotaryWhole) their first pair (255: not rotated).
+  uint8_t lo[16], hi[16], first_pair[16];
   int pairs, pair_end[3];          // rotated pairs; where each axis's pairs end
   int grid_h, grid_w, start[3];
   float eps, inv_count[2], mult;
@@ -71,10 +75,10 @@ template <typename T> __device__ __forceinline__ void times_weights(float (&f)[8
 }
 
 template <typename T, int NORM, int ROT>
-__global__ void __launch_bounds__(kThreads, 3)
+__global__ void __launch_bounds__(kThreads, 2)
 qk_norm_kernel(const __grid_constant__ QkArgs a) {
   extern __shared__ float2 tab[];                       // [tokens of the CTA][pairs]
-  __shared__ float xch[ROT == VC_ROTARY_HALF ? kThreads * 8 + 1 : 1];   // (the last one is 0)
+  __shared__ float xch[ROT == VC_ROTARY_HALF ? kThreads * 16 + 1 : 1];  // (the last one is 0)
   __shared__ float part[2][NORM == VC_NORM_TOKEN ? kThreads / 32 : 1];
   constexpr int kKeep = heads_held(sizeof(T), ROT);
   const int lanes = 1 << a.log_lanes, tokens = kThreads >> (a.log_lanes + a.log_hl);
@@ -82,12 +86,16 @@ qk_norm_kernel(const __grid_constant__ QkArgs a) {
   const int b = blockIdx.y, n0 = blockIdx.x * tokens * a.turns_taken;
   const int t = blockIdx.z + a.first, H = a.H[t];       // Q or K
   const void* w = a.w[t];
-  // My heads are hl, hl + hls, ...: kKeep of them are loaded at a time.  (A thread without a token or a channel reads the last
-  // one's and stores nothing.)
-  const int64_t sx = a.in[t].h << a.log_hl, sy = a.out[t].h << a.log_hl, xn = a.in[t].n;
-  const T* xb = static_cast<const T*>(a.x[t]) + (b * a.in[t].b + 8 * min(c, a.chunks - 1));
-  T* yb = static_cast<T*>(a.y[t]) + (b * a.out[t].b + hl * a.out[t].h + (int64_t)(n0 + tt) * a.out[t].n + 8 * c);
-  const int64_t w_at0 = ((int64_t)hl * a.chunks + min(c, a.chunks - 1)) * 8;
+  // My channels: two groups of eight.  My heads: hl, hl + hls, ..., `rows` of them, the last one perhaps
+  // behind H.  (What lies outside reads another place and is neither summed nor stored.)
+  const int rows = (H + (1 << a.log_hl) - 1) >> a.log_hl;
+  const int lo = a.lo[c], hi = a.hi[c];
+  const bool ch0 = lo != 255, ch1 = hi != 255, last_in = hl + ((rows - 1) << a.log_hl) < H;
+  const int64_t sx = a.in[t].h << a.log_hl, sy = a.out[t].h << a.log_hl, xn = a.in[t].n, yn = a.out[t].n * tokens;
+  const int at0 = 8 * (ch0 ? lo : 0), at1 = 8 * (ch1 ? hi : 0);
+  const T* xb = static_cast<const T*>(a.x[t]) + (b * a.in[t].b + (hl < H ? hl : 0) * a.in[t].h + at0);
+  T* yb = static_cast<T*>(a.y[t]) + (b * a.out[t].b + hl * a.out[t].h + (int64_t)(n0 + tt) * a.out[t].n + at0);
+  const int step = at1 - at0;
 
   auto lanes_sum = [](float v, int count) {
     for (int s = count >> 1; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
@@ -105,52 +113,53 @@ qk_norm_kernel(const __grid_constant__ QkArgs a) {
     sm100::unpack2(s, even, odd);
     return even + odd;
   };
-  float wt[8];
+  float wt[2][8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) wt[e] = 1.f;
-  if (NORM == VC_NORM_HEAD && w && c < a.chunks) times_weights<T>(wt, a, w, 8 * c);
+  for (int e = 0; e < 8; ++e) wt[0][e] = wt[1][e] = 1.f;
+  if (NORM == VC_NORM_HEAD && w) {
+    times_weights<T>(wt[0], a, w, at0);
+    times_weights<T>(wt[1], a, w, at1);
+  }
 
   pdl_wait();
-  // The angles of all tokens at once: every lane has one to form.  The first tokens' heads are on their way meanwhile.
-  Raw8<T> raw[kKeep];
-  auto load_heads = [&](int n, int h0) {
-    const T* x0 = xb + (int64_t)min(n, a.N - 1) * xn;
-    const T* from = x0 + hl * a.in[t].h + (h0 >> a.log_hl) * sx;
+  Raw8<T> raw[kKeep][2];
+  auto load_rows = [&](int n, int i0) {                 // heads i0, i0 + 1, ... of mine
+    const T* from = xb + (int64_t)min(n, a.N - 1) * xn + i0 * sx;
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
-      const int h = h0 + (i << a.log_hl);
-      if (h >= H) break;
-      raw[i].load(h + hl < H ? from : x0);
+      if (i0 + i >= rows) break;
+      if (i0 + i + 1 == rows && !last_in) from = xb + (int64_t)min(n, a.N - 1) * xn;
+      raw[i][0].load(from);
+      raw[i][1].load(from + step);
       from += sx;
     }
   };
-  load_heads(n0 + tt, 0);
+  // The angles of all tokens at once: every lane has one to form.  The first tokens' heads are on their way meanwhile.
+  load_rows(n0 + tt, 0);
   if constexpr (ROT != VC_ROTARY_NONE) fill_table(a, tab, b, n0, tokens * a.turns_taken);
-  if (ROT == VC_ROTARY_HALF && threadIdx.x == 0) xch[kThreads * 8] = 0.f;
+  if (ROT == VC_ROTARY_HALF && threadIdx.x == 0) xch[kThreads * 16] = 0.f;
   if constexpr (ROT != VC_ROTARY_NONE && NORM != VC_NORM_TOKEN) __syncthreads();
 
   for (int turn = 0; turn < a.turns_taken; ++turn) {
     const int n = n0 + turn * tokens + tt;
     if (n - tt >= a.N) break;
-    const bool live = n < a.N && c < a.chunks;
-    if (turn) load_heads(n, 0);
+    const bool live0 = n < a.N && ch0, live1 = n < a.N && ch1;
+    if (turn) load_rows(n, 0);
     float inv = 1.f;
     if constexpr (NORM == VC_NORM_TOKEN) {
-      float ss = 0.f;
-      for (int h0 = 0;;) {
+      float ss0 = 0.f, ss1 = 0.f;
+      for (int i0 = 0;;) {
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
-          const int h = h0 + (i << a.log_hl);
-          if (h >= H) break;
-          const float sq = squares(raw[i]);
-          ss += h + hl < H ? sq : 0.f;
+          if (i0 + i >= rows) break;
+          const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
+          if (i0 + i + 1 < rows || last_in) { ss0 += q0; ss1 += q1; }
         }
-        h0 += kKeep << a.log_hl;
-        if (h0 >= H) break;
-        load_heads(n, h0);
+        i0 += kKeep;
+        if (i0 >= rows) break;
+        load_rows(n, i0);
       }
-      if (c >= a.chunks) ss = 0.f;
-      ss = lanes_sum(ss, min(lanes << a.log_hl, 32));                    // a token's lanes in this warp
+      float ss = lanes_sum((ch0 ? ss0 : 0.f) + (ch1 ? ss1 : 0.f), min(lanes << a.log_hl, 32));   // a token's lanes in this warp
       if ((threadIdx.x & 31) == 0) part[turn & 1][threadIdx.x >> 5] = ss;
       __syncthreads();
       const int warps = lanes << a.log_hl >> 5;                          // of a token; 0 or 1: its sum is at hand
@@ -159,94 +168,135 @@ qk_norm_kernel(const __grid_constant__ QkArgs a) {
         for (int i = 0; i < warps; ++i) ss += part[turn & 1][(threadIdx.x >> 5 & -warps) + i];   // one order for every thread of the token
       }
       inv = rsqrtf(fmaf(ss, a.inv_count[t], a.eps));
-      if (H > kKeep << a.log_hl) load_heads(n, 0);                       // more heads than the registers hold: read twice
+      if (rows > kKeep) load_rows(n, 0);                                 // more heads than the registers hold: read twice
     }
 
     // cos and sin of my channels.  One that is not rotated keeps its value whatever its neighbour holds: bit e of `still`, or 0 in the
-    // place of the other half (with eight bits to test the predicate registers run out).
-    constexpr int kAngles = ROT == VC_ROTARY_HALF ? 8 : 4;
-    float cs[kAngles], sn[kAngles];
-    int src[ROT == VC_ROTARY_HALF ? 8 : 1];
+    // place of the other half (with as many bits to test the predicate registers run out).
+    constexpr int kAngles = ROT >= VC_ROTARY_HALF ? 8 : 4;
+    float cs[2][kAngles], sn[2][kAngles];
+    int src[2][ROT == VC_ROTARY_HALF ? 8 : 1];
     uint32_t still = 0;
-    if constexpr (ROT != VC_ROTARY_NONE) {
-      const float2* mine = tab + (turn * tokens + tt) * a.pairs;
+    const float2* mine = tab + (turn * tokens + tt) * a.pairs;
+    const bool turned = ROT == kRotaryWhole && a.first_pair[c] != 255;
+    if constexpr (ROT == kRotaryWhole) {
+      const float4* from = reinterpret_cast<const float4*>(mine + (turned ? a.first_pair[c] : 0));      // (a multiple of eight pairs on)
 #pragma unroll
-      for (int e = 0; e < kAngles; ++e) {
-        cs[e] = 1.f; sn[e] = 0.f;
-        if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
-          const int p = 4 * c + e;
-          if (p < a.pairs) { cs[e] = mine[p].x; sn[e] = mine[p].y; } else still |= 1u << e;
-        } else {
-          const int ch = 8 * c + e;
-          src[e] = kThreads * 8 - r * 8 * lanes;
-          if (ch < 2 * a.pairs) {
-            const int axis = (ch >= 2 * a.pair_end[0]) + (ch >= 2 * a.pair_end[1]);
-            const int p0 = axis ? a.pair_end[axis - 1] : 0, half = a.pair_end[axis] - p0, i = ch - 2 * p0;
-            const bool low = i < half;
-            const int other = low ? ch + half : ch - half;
-            const float2 cosine_sine = mine[p0 + (low ? i : i - half)];
-            cs[e] = cosine_sine.x; sn[e] = low ? -cosine_sine.y : cosine_sine.y;
-            src[e] = (other & 7) * lanes + (other >> 3);
+      for (int e = 0; e < 4; ++e) {
+        const float4 v = from[e];
+        cs[0][2 * e] = v.x; sn[0][2 * e] = v.y; cs[0][2 * e + 1] = v.z; sn[0][2 * e + 1] = v.w;
+      }
+    } else if constexpr (ROT != VC_ROTARY_NONE) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int cq = c + q * lanes;
+#pragma unroll
+        for (int e = 0; e < kAngles; ++e) {
+          cs[q][e] = 1.f; sn[q][e] = 0.f;
+          if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
+            const int p = 4 * cq + e;
+            if (p < a.pairs) { cs[q][e] = mine[p].x; sn[q][e] = mine[p].y; } else still |= 1u << (4 * q + e);
+          } else {
+            const int ch = 8 * cq + e;
+            src[q][e] = kThreads * 16 - r * 16 * lanes;
+            if (ch < 2 * a.pairs) {
+              const int axis = (ch >= 2 * a.pair_end[0]) + (ch >= 2 * a.pair_end[1]);
+              const int p0 = axis ? a.pair_end[axis - 1] : 0, half = a.pair_end[axis] - p0, i = ch - 2 * p0;
+              const bool low = i < half;
+              const int other = low ? ch + half : ch - half;
+              const float2 cosine_sine = mine[p0 + (low ? i : i - half)];
+              cs[q][e] = cosine_sine.x; sn[q][e] = low ? -cosine_sine.y : cosine_sine.y;
+              src[q][e] = (other & 7) * 2 * lanes + (other >> 3);
+            }
           }
         }
       }
     }
-    auto rotate = [&](float (&f)[8]) {
-      if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
-        float g[8];
+    auto rotate = [&](float (&f)[2][8]) {
+      if constexpr (ROT == kRotaryWhole) {
+        if (turned) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          g[2 * e] = f[2 * e] * cs[e] - f[2 * e + 1] * sn[e];
-          g[2 * e + 1] = f[2 * e] * sn[e] + f[2 * e + 1] * cs[e];
+          for (int e = 0; e < 8; ++e) {
+            const float f0 = f[0][e], f1 = f[1][e];
+            f[0][e] = f0 * cs[0][e] - f1 * sn[0][e];
+            f[1][e] = f0 * sn[0][e] + f1 * cs[0][e];
+          }
         }
-        if (a.partial) {
+      } else if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (still >> (e / 2) & 1) g[e] = f[e];
+        for (int q = 0; q < 2; ++q) {
+          float g[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            g[2 * e] = f[q][2 * e] * cs[q][e] - f[q][2 * e + 1] * sn[q][e];
+            g[2 * e + 1] = f[q][2 * e] * sn[q][e] + f[q][2 * e + 1] * cs[q][e];
+          }
+          if (a.partial) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (still >> (4 * q + e / 2) & 1) g[e] = f[q][e];
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[q][e] = g[e];
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = g[e];
       } else if constexpr (ROT == VC_ROTARY_HALF) {
         // a pair's halves are half an axis apart, in another lane as a rule: the head's channels change places in
         // shared memory, element-major so that the lanes of an access lie side by side
-        float* row = xch + r * 8 * lanes;
+        float* row = xch + r * 16 * lanes;
         __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) row[e * lanes + c] = f[e];
+        for (int e = 0; e < 8; ++e) {
+          row[e * 2 * lanes + c] = f[0][e];
+          row[e * 2 * lanes + c + lanes] = f[1][e];
+        }
         __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = f[e] * cs[e] + row[src[e]] * sn[e];
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[q][e] = f[q][e] * cs[q][e] + row[src[q][e]] * sn[q][e];
       }
     };
 
     T* y = yb;
-    int64_t w_at = w_at0;
-    for (int h0 = 0; h0 < H;) {
+    int64_t w_at = (int64_t)hl * a.chunks * 8 + at0;
+    for (int i0 = 0; i0 < rows;) {
 #pragma unroll
       for (int i = 0; i < kKeep; ++i) {
-        const int h = h0 + (i << a.log_hl);
-        if (h >= H) break;
-        const bool mine = live && h + hl < H;
-        float f[8];
-        raw[i].get(f);
+        if (i0 + i >= rows) break;
+        const bool in = i0 + i + 1 < rows || last_in;
+        float f[2][8];
+        raw[i][0].get(f[0]);
+        raw[i][1].get(f[1]);
         if constexpr (NORM == VC_NORM_HEAD) {
-          const float sq = squares(raw[i]);
-          times(f, rsqrtf(fmaf(lanes_sum(c < a.chunks ? sq : 0.f, lanes), a.inv_count[t], a.eps)));
-          times(f, wt);
+          const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
+          inv = rsqrtf(fmaf(lanes_sum((ch0 ? q0 : 0.f) + (ch1 ? q1 : 0.f), lanes), a.inv_count[t], a.eps));
+        }
+        if constexpr (NORM != VC_NORM_NONE) {
+          times(f[0], inv);
+          times(f[1], inv);
+        }
+        if constexpr (NORM == VC_NORM_HEAD) {
+          times(f[0], wt[0]);
+          times(f[1], wt[1]);
         }
         if constexpr (NORM == VC_NORM_TOKEN) {
-          times(f, inv);
-          if (w && mine) times_weights<T>(f, a, w, w_at);
+          if (w && in) {
+            times_weights<T>(f[0], a, w, w_at);
+            times_weights<T>(f[1], a, w, w_at + step);
+          }
           w_at += (int64_t)a.chunks * 8 << a.log_hl;
         }
         rotate(f);
-        if (mine) store8<T>(y, f);
+        if (in) {
+          if (live0) store8<T>(y, f[0]);
+          if (live1) store8<T>(y + step, f[1]);
+        }
         y += sy;
       }
-      h0 += kKeep << a.log_hl;
-      if (h0 < H) load_heads(n, h0);
+      i0 += kKeep;
+      if (i0 < rows) load_rows(n, i0);
     }
-    yb += tokens * a.out[t].n;
+    yb += yn;
   }
 }
 
@@ -254,6 +304,7 @@ template <typename T, int NORM>
 cudaError_t launch_rot(int rot, const QkArgs& a, dim3 grid, size_t smem, cudaStream_t s) {
   if (rot == VC_ROTARY_NONE) return launch_overlapped(qk_norm_kernel<T, NORM, VC_ROTARY_NONE>, grid, kThreads, smem, s, a);
   if (rot == VC_ROTARY_INTERLEAVED) return launch_overlapped(qk_norm_kernel<T, NORM, VC_ROTARY_INTERLEAVED>, grid, kThreads, smem, s, a);
+  if (rot == kRotaryWhole) return launch_overlapped(qk_norm_kernel<T, NORM, kRotaryWhole>, grid, kThreads, smem, s, a);
   return launch_overlapped(qk_norm_kernel<T, NORM, VC_ROTARY_HALF>, grid, kThreads, smem, s, a);
 }
 template <typename T>
@@ -265,14 +316,15 @@ cudaError_t launch_norm(int norm, int rot, const QkArgs& a, dim3 grid, size_t sm
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
-// Frequencies of an axis's pairs in turns per position.  Powers by repeated multiplication in extended precision: 64 steps
-// of 2^-64 each, against one call of pow() per pair (a call's host time: 1.1 us instead of 4.6 for 64 pairs).
+// Frequencies of an axis's pairs in turns per position.  Powers by repeated multiplication, one call of pow() instead of one a pair
+// (1 us of a call's host time instead of 4): after i steps they are off by i / 2 units of 2^-52, but by then the frequency itself
+// has fallen so far that no angle is off by more than that of the first pairs.
 bool axis_frequencies(const vc_qk_params* p, int n, double factor, int original, double theta, double* out) {
   if (n == 0) return true;
   const int pairs = n / 2;
   if (p->rope_scaling == VC_ROPE_SCALING_NTK && n > 2) theta *= std::pow(factor, (double)n / (n - 2));
   if (!(theta > 0.0) || !std::isfinite(theta)) return false;
-  const long double ratio = std::pow((long double)theta, -2.0L / n);
+  const double ratio = std::pow(theta, -2.0 / n);
   double lo = 0, hi = 1;
   if (p->rope_scaling == VC_ROPE_SCALING_YARN) {
     const double fast = p->yarn_beta_fast != 0.f ? p->yarn_beta_fast : 32.0, slow = p->yarn_beta_slow != 0.f ? p->yarn_beta_slow : 1.0;
@@ -283,9 +335,9 @@ bool axis_frequencies(const vc_qk_params* p, int n, double factor, int original,
     hi = hi < n - 1 ? hi : n - 1;
     if (hi - lo < 0.001) hi = lo + 0.001;
   }
-  long double f = 1.0L / (long double)kTwoPi;
+  double f = 1.0 / kTwoPi;
   for (int i = 0; i < pairs; ++i, f *= ratio) {
-    double v = (double)f;
+    double v = f;
     if (p->rope_scaling == VC_ROPE_SCALING_LINEAR) v /= factor;
     if (p->rope_scaling == VC_ROPE_SCALING_YARN) {
       double r = (i - lo) / (hi - lo);
@@ -368,6 +420,7 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
     }
     a.positions = positions;
     if (pairs == 0) rot = VC_ROTARY_NONE;
+    if (rot == VC_ROTARY_HALF && dims[0] % 16 == 0 && dims[1] % 16 == 0 && dims[2] % 16 == 0) rot = kRotaryWhole;
   }
   a.N = p->N;
   a.chunks = p->d / 8;
@@ -375,7 +428,27 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
   a.partial = 2 * a.pairs < p->d;
   a.weight_dtype = p->weight_dtype;
   a.eps = p->eps != 0.f ? p->eps : 1e-6f;
-  while ((1 << a.log_lanes) < a.chunks) ++a.log_lanes;
+  while ((2 << a.log_lanes) < a.chunks) ++a.log_lanes;
+  for (int i = 0; i < 16; ++i) {
+    const int lanes = 1 << a.log_lanes;
+    a.lo[i] = (uint8_t)(i < lanes && i < a.chunks ? i : 255);
+    a.hi[i] = (uint8_t)(i < lanes && i + lanes < a.chunks ? i + lanes : 255);
+    a.first_pair[i] = 255;
+  }
+  if (rot == kRotaryWhole) {                 // lanes for the pairs of every axis, then for the channels behind them
+    int lane = 0, chunk = 0, pair = 0;
+    for (int axis = 0; axis < 3; ++axis) {
+      const int groups = (a.pair_end[axis] - pair) / 8;
+      for (int i = 0; i < groups; ++i, ++lane, pair += 8) {
+        a.lo[lane] = (uint8_t)(chunk + i); a.hi[lane] = (uint8_t)(chunk + groups + i); a.first_pair[lane] = (uint8_t)pair;
+      }
+      chunk += 2 * groups;
+    }
+    for (; lane < 16; ++lane, chunk += 2) {
+      a.lo[lane] = (uint8_t)(chunk < a.chunks ? chunk : 255); a.hi[lane] = (uint8_t)(chunk + 1 < a.chunks ? chunk + 1 : 255);
+      a.first_pair[lane] = 255;
+    }
+  }
   const int rows = kThreads >> a.log_lanes, heads = a.H[0] > a.H[1] ? a.H[0] : a.H[1], keep = heads_held(es, rot);
   const int tensors = (a.H[0] > 0) + (a.H[1] > 0);
   a.first = a.H[0] == 0;
