@@ -13,11 +13,11 @@ namespace {
 
 using namespace layer;
 
-constexpr int kThreads = 256, kMaxPairs = 128;
+constexpr int kThreads = 128, kMaxPairs = 128;
 // Halves whose axes are multiples of 16 channels: a pair's two channels lie in whole groups of eight, and one thread owns both groups.
 constexpr int kRotaryWhole = VC_ROTARY_HALF + 1;
 
-// Heads whose channels a thread holds in registers: two CTAs an SM then fit the register file.
+// Heads whose channels a thread holds in registers: four CTAs an SM then fit the register file.
 __host__ __device__ constexpr int heads_held(int elem_bytes, int rotary) { return rotary == VC_ROTARY_HALF ? (elem_bytes == 2 ? 3 : 1) : (elem_bytes == 2 ? 5 : 2); }
 
 struct QkArgs {
@@ -27,7 +27,6 @@ struct QkArgs {
   vc_strides in[2], out[2];
   int H[2], first;                 // first: 1 if there is no Q
   int N, chunks, log_lanes, log_hl, log_pairs, weight_dtype;     // log_pairs: 2^log_pairs >= pairs
-  int turns_taken;                 // a CTA takes that many groups of tokens, one behind the other
   bool same_type;                  // weights are of the tensors' type
   bool partial;                    // some channels are not rotated
   // The two groups of eight channels of a lane (255: none), and (kRotaryWhole) their first pair (255: not rotated).
@@ -75,15 +74,15 @@ template <typename T> __device__ __forceinline__ void times_weights(float (&f)[8
 }
 
 template <typename T, int NORM, int ROT>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, 4)
 qk_norm_kernel(const __grid_constant__ QkArgs a) {
   extern __shared__ float2 tab[];                       // [tokens of the CTA][pairs]
   __shared__ float xch[ROT == VC_ROTARY_HALF ? kThreads * 16 + 1 : 1];  // (the last one is 0)
-  __shared__ float part[2][NORM == VC_NORM_TOKEN ? kThreads / 32 : 1];
+  __shared__ float part[NORM == VC_NORM_TOKEN ? kThreads / 32 : 1];
   constexpr int kKeep = heads_held(sizeof(T), ROT);
   const int lanes = 1 << a.log_lanes, tokens = kThreads >> (a.log_lanes + a.log_hl);
   const int c = threadIdx.x & (lanes - 1), r = threadIdx.x >> a.log_lanes, hl = r & ((1 << a.log_hl) - 1), tt = r >> a.log_hl;
-  const int b = blockIdx.y, n0 = blockIdx.x * tokens * a.turns_taken;
+  const int b = blockIdx.y, n0 = blockIdx.x * tokens, n = n0 + tt;
   const int t = blockIdx.z + a.first, H = a.H[t];       // Q or K
   const void* w = a.w[t];
   // My channels: two groups of eight.  My heads: hl, hl + hls, ..., `rows` of them, the last one perhaps
@@ -91,10 +90,10 @@ qk_norm_kernel(const __grid_constant__ QkArgs a) {
   const int rows = (H + (1 << a.log_hl) - 1) >> a.log_hl;
   const int lo = a.lo[c], hi = a.hi[c];
   const bool ch0 = lo != 255, ch1 = hi != 255, last_in = hl + ((rows - 1) << a.log_hl) < H;
-  const int64_t sx = a.in[t].h << a.log_hl, sy = a.out[t].h << a.log_hl, xn = a.in[t].n, yn = a.out[t].n * tokens;
+  const int64_t sx = a.in[t].h << a.log_hl, sy = a.out[t].h << a.log_hl;
   const int at0 = 8 * (ch0 ? lo : 0), at1 = 8 * (ch1 ? hi : 0);
-  const T* xb = static_cast<const T*>(a.x[t]) + (b * a.in[t].b + (hl < H ? hl : 0) * a.in[t].h + at0);
-  T* yb = static_cast<T*>(a.y[t]) + (b * a.out[t].b + hl * a.out[t].h + (int64_t)(n0 + tt) * a.out[t].n + at0);
+  const T* x = static_cast<const T*>(a.x[t]) + (b * a.in[t].b + (hl < H ? hl : 0) * a.in[t].h + (int64_t)min(n, a.N - 1) * a.in[t].n + at0);
+  T* y = static_cast<T*>(a.y[t]) + (b * a.out[t].b + hl * a.out[t].h + (int64_t)n * a.out[t].n + at0);
   const int step = at1 - at0;
 
   auto lanes_sum = [](float v, int count) {
@@ -113,6 +112,20 @@ qk_norm_kernel(const __grid_constant__ QkArgs a) {
     sm100::unpack2(s, even, odd);
     return even + odd;
   };
+  pdl_wait();
+  Raw8<T> raw[kKeep][2];
+  auto load_rows = [&](int i0) {                        // heads i0, i0 + 1, ... of mine
+    const T* from = x + i0 * sx;
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+      if (i0 + i >= rows) break;
+      if (i0 + i + 1 == rows && !last_in) from = x;
+      raw[i][0].load(from);
+      raw[i][1].load(from + step);
+      from += sx;
+    }
+  };
+  load_rows(0);                                         // (on their way while the angles are formed)
   float wt[2][8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) wt[0][e] = wt[1][e] = 1.f;
@@ -120,183 +133,160 @@ qk_norm_kernel(const __grid_constant__ QkArgs a) {
     times_weights<T>(wt[0], a, w, at0);
     times_weights<T>(wt[1], a, w, at1);
   }
-
-  pdl_wait();
-  Raw8<T> raw[kKeep][2];
-  auto load_rows = [&](int n, int i0) {                 // heads i0, i0 + 1, ... of mine
-    const T* from = xb + (int64_t)min(n, a.N - 1) * xn + i0 * sx;
-#pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      if (i0 + i >= rows) break;
-      if (i0 + i + 1 == rows && !last_in) from = xb + (int64_t)min(n, a.N - 1) * xn;
-      raw[i][0].load(from);
-      raw[i][1].load(from + step);
-      from += sx;
-    }
-  };
-  // The angles of all tokens at once: every lane has one to form.  The first tokens' heads are on their way meanwhile.
-  load_rows(n0 + tt, 0);
-  if constexpr (ROT != VC_ROTARY_NONE) fill_table(a, tab, b, n0, tokens * a.turns_taken);
+  if constexpr (ROT != VC_ROTARY_NONE) fill_table(a, tab, b, n0, tokens);
   if (ROT == VC_ROTARY_HALF && threadIdx.x == 0) xch[kThreads * 16] = 0.f;
   if constexpr (ROT != VC_ROTARY_NONE && NORM != VC_NORM_TOKEN) __syncthreads();
 
-  for (int turn = 0; turn < a.turns_taken; ++turn) {
-    const int n = n0 + turn * tokens + tt;
-    if (n - tt >= a.N) break;
-    const bool live0 = n < a.N && ch0, live1 = n < a.N && ch1;
-    if (turn) load_rows(n, 0);
-    float inv = 1.f;
-    if constexpr (NORM == VC_NORM_TOKEN) {
-      float ss0 = 0.f, ss1 = 0.f;
-      for (int i0 = 0;;) {
-#pragma unroll
-        for (int i = 0; i < kKeep; ++i) {
-          if (i0 + i >= rows) break;
-          const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
-          if (i0 + i + 1 < rows || last_in) { ss0 += q0; ss1 += q1; }
-        }
-        i0 += kKeep;
-        if (i0 >= rows) break;
-        load_rows(n, i0);
-      }
-      float ss = lanes_sum((ch0 ? ss0 : 0.f) + (ch1 ? ss1 : 0.f), min(lanes << a.log_hl, 32));   // a token's lanes in this warp
-      if ((threadIdx.x & 31) == 0) part[turn & 1][threadIdx.x >> 5] = ss;
-      __syncthreads();
-      const int warps = lanes << a.log_hl >> 5;                          // of a token; 0 or 1: its sum is at hand
-      if (warps > 1) {
-        ss = 0.f;
-        for (int i = 0; i < warps; ++i) ss += part[turn & 1][(threadIdx.x >> 5 & -warps) + i];   // one order for every thread of the token
-      }
-      inv = rsqrtf(fmaf(ss, a.inv_count[t], a.eps));
-      if (rows > kKeep) load_rows(n, 0);                                 // more heads than the registers hold: read twice
-    }
-
-    // cos and sin of my channels.  One that is not rotated keeps its value whatever its neighbour holds: bit e of `still`, or 0 in the
-    // place of the other half (with as many bits to test the predicate registers run out).
-    constexpr int kAngles = ROT >= VC_ROTARY_HALF ? 8 : 4;
-    float cs[2][kAngles], sn[2][kAngles];
-    int src[2][ROT == VC_ROTARY_HALF ? 8 : 1];
-    uint32_t still = 0;
-    const float2* mine = tab + (turn * tokens + tt) * a.pairs;
-    const bool turned = ROT == kRotaryWhole && a.first_pair[c] != 255;
-    if constexpr (ROT == kRotaryWhole) {
-      const float4* from = reinterpret_cast<const float4*>(mine + (turned ? a.first_pair[c] : 0));      // (a multiple of eight pairs on)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float4 v = from[e];
-        cs[0][2 * e] = v.x; sn[0][2 * e] = v.y; cs[0][2 * e + 1] = v.z; sn[0][2 * e + 1] = v.w;
-      }
-    } else if constexpr (ROT != VC_ROTARY_NONE) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int cq = c + q * lanes;
-#pragma unroll
-        for (int e = 0; e < kAngles; ++e) {
-          cs[q][e] = 1.f; sn[q][e] = 0.f;
-          if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
-            const int p = 4 * cq + e;
-            if (p < a.pairs) { cs[q][e] = mine[p].x; sn[q][e] = mine[p].y; } else still |= 1u << (4 * q + e);
-          } else {
-            const int ch = 8 * cq + e;
-            src[q][e] = kThreads * 16 - r * 16 * lanes;
-            if (ch < 2 * a.pairs) {
-              const int axis = (ch >= 2 * a.pair_end[0]) + (ch >= 2 * a.pair_end[1]);
-              const int p0 = axis ? a.pair_end[axis - 1] : 0, half = a.pair_end[axis] - p0, i = ch - 2 * p0;
-              const bool low = i < half;
-              const int other = low ? ch + half : ch - half;
-              const float2 cosine_sine = mine[p0 + (low ? i : i - half)];
-              cs[q][e] = cosine_sine.x; sn[q][e] = low ? -cosine_sine.y : cosine_sine.y;
-              src[q][e] = (other & 7) * 2 * lanes + (other >> 3);
-            }
-          }
-        }
-      }
-    }
-    auto rotate = [&](float (&f)[2][8]) {
-      if constexpr (ROT == kRotaryWhole) {
-        if (turned) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float f0 = f[0][e], f1 = f[1][e];
-            f[0][e] = f0 * cs[0][e] - f1 * sn[0][e];
-            f[1][e] = f0 * sn[0][e] + f1 * cs[0][e];
-          }
-        }
-      } else if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          float g[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            g[2 * e] = f[q][2 * e] * cs[q][e] - f[q][2 * e + 1] * sn[q][e];
-            g[2 * e + 1] = f[q][2 * e] * sn[q][e] + f[q][2 * e + 1] * cs[q][e];
-          }
-          if (a.partial) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (still >> (4 * q + e / 2) & 1) g[e] = f[q][e];
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[q][e] = g[e];
-        }
-      } else if constexpr (ROT == VC_ROTARY_HALF) {
-        // a pair's halves are half an axis apart, in another lane as a rule: the head's channels change places in
-        // shared memory, element-major so that the lanes of an access lie side by side
-        float* row = xch + r * 16 * lanes;
-        __syncwarp();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          row[e * 2 * lanes + c] = f[0][e];
-          row[e * 2 * lanes + c + lanes] = f[1][e];
-        }
-        __syncwarp();
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[q][e] = f[q][e] * cs[q][e] + row[src[q][e]] * sn[q][e];
-      }
-    };
-
-    T* y = yb;
-    int64_t w_at = (int64_t)hl * a.chunks * 8 + at0;
-    for (int i0 = 0; i0 < rows;) {
+  const bool live0 = n < a.N && ch0, live1 = n < a.N && ch1;
+  float inv = 1.f;
+  if constexpr (NORM == VC_NORM_TOKEN) {
+    float ss0 = 0.f, ss1 = 0.f;
+    for (int i0 = 0;;) {
 #pragma unroll
       for (int i = 0; i < kKeep; ++i) {
         if (i0 + i >= rows) break;
-        const bool in = i0 + i + 1 < rows || last_in;
-        float f[2][8];
-        raw[i][0].get(f[0]);
-        raw[i][1].get(f[1]);
-        if constexpr (NORM == VC_NORM_HEAD) {
-          const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
-          inv = rsqrtf(fmaf(lanes_sum((ch0 ? q0 : 0.f) + (ch1 ? q1 : 0.f), lanes), a.inv_count[t], a.eps));
-        }
-        if constexpr (NORM != VC_NORM_NONE) {
-          times(f[0], inv);
-          times(f[1], inv);
-        }
-        if constexpr (NORM == VC_NORM_HEAD) {
-          times(f[0], wt[0]);
-          times(f[1], wt[1]);
-        }
-        if constexpr (NORM == VC_NORM_TOKEN) {
-          if (w && in) {
-            times_weights<T>(f[0], a, w, w_at);
-            times_weights<T>(f[1], a, w, w_at + step);
-          }
-          w_at += (int64_t)a.chunks * 8 << a.log_hl;
-        }
-        rotate(f);
-        if (in) {
-          if (live0) store8<T>(y, f[0]);
-          if (live1) store8<T>(y + step, f[1]);
-        }
-        y += sy;
+        const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
+        if (i0 + i + 1 < rows || last_in) { ss0 += q0; ss1 += q1; }
       }
       i0 += kKeep;
-      if (i0 < rows) load_rows(n, i0);
+      if (i0 >= rows) break;
+      load_rows(i0);
     }
-    yb += yn;
+    float ss = lanes_sum((ch0 ? ss0 : 0.f) + (ch1 ? ss1 : 0.f), min(lanes << a.log_hl, 32));   // a token's lanes in this warp
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = ss;
+    __syncthreads();
+    const int warps = lanes << a.log_hl >> 5;                          // of a token; 0 or 1: its sum is at hand
+    if (warps > 1) {
+      ss = 0.f;
+      for (int i = 0; i < warps; ++i) ss += part[(threadIdx.x >> 5 & -warps) + i];   // one order for every thread of the token
+    }
+    inv = rsqrtf(fmaf(ss, a.inv_count[t], a.eps));
+    if (rows > kKeep) load_rows(0);                                 // more heads than the registers hold: read twice
+  }
+
+  // cos and sin of my channels.  One that is not rotated keeps its value whatever its neighbour holds: bit e of `still`, or 0 in the
+  // place of the other half (with as many bits to test the predicate registers run out).
+  constexpr int kAngles = ROT >= VC_ROTARY_HALF ? 8 : 4;
+  float cs[2][kAngles], sn[2][kAngles];
+  int src[2][ROT == VC_ROTARY_HALF ? 8 : 1];
+  uint32_t still = 0;
+  const float2* mine = tab + tt * a.pairs;
+  const bool turned = ROT == kRotaryWhole && a.first_pair[c] != 255;
+  if constexpr (ROT == kRotaryWhole) {
+    const float4* from = reinterpret_cast<const float4*>(mine + (turned ? a.first_pair[c] : 0));      // (a multiple of eight pairs on)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float4 v = from[e];
+      cs[0][2 * e] = v.x; sn[0][2 * e] = v.y; cs[0][2 * e + 1] = v.z; sn[0][2 * e + 1] = v.w;
+    }
+  } else if constexpr (ROT != VC_ROTARY_NONE) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int cq = c + q * lanes;
+#pragma unroll
+      for (int e = 0; e < kAngles; ++e) {
+        cs[q][e] = 1.f; sn[q][e] = 0.f;
+        if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
+          const int p = 4 * cq + e;
+          if (p < a.pairs) { cs[q][e] = mine[p].x; sn[q][e] = mine[p].y; } else still |= 1u << (4 * q + e);
+        } else {
+          const int ch = 8 * cq + e;
+          src[q][e] = kThreads * 16 - r * 16 * lanes;
+          if (ch < 2 * a.pairs) {
+            const int axis = (ch >= 2 * a.pair_end[0]) + (ch >= 2 * a.pair_end[1]);
+            const int p0 = axis ? a.pair_end[axis - 1] : 0, half = a.pair_end[axis] - p0, i = ch - 2 * p0;
+            const bool low = i < half;
+            const int other = low ? ch + half : ch - half;
+            const float2 cosine_sine = mine[p0 + (low ? i : i - half)];
+            cs[q][e] = cosine_sine.x; sn[q][e] = low ? -cosine_sine.y : cosine_sine.y;
+            src[q][e] = (other & 7) * 2 * lanes + (other >> 3);
+          }
+        }
+      }
+    }
+  }
+  auto rotate = [&](float (&f)[2][8]) {
+    if constexpr (ROT == kRotaryWhole) {
+      if (turned) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float f0 = f[0][e], f1 = f[1][e];
+          f[0][e] = f0 * cs[0][e] - f1 * sn[0][e];
+          f[1][e] = f0 * sn[0][e] + f1 * cs[0][e];
+        }
+      }
+    } else if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        float g[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          g[2 * e] = f[q][2 * e] * cs[q][e] - f[q][2 * e + 1] * sn[q][e];
+          g[2 * e + 1] = f[q][2 * e] * sn[q][e] + f[q][2 * e + 1] * cs[q][e];
+        }
+        if (a.partial) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (still >> (4 * q + e / 2) & 1) g[e] = f[q][e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[q][e] = g[e];
+      }
+    } else if constexpr (ROT == VC_ROTARY_HALF) {
+      // a pair's halves are half an axis apart, in another lane as a rule: the head's channels change places in
+      // shared memory, element-major so that the lanes of an access lie side by side
+      float* row = xch + r * 16 * lanes;
+      __syncwarp();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        row[e * 2 * lanes + c] = f[0][e];
+        row[e * 2 * lanes + c + lanes] = f[1][e];
+      }
+      __syncwarp();
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[q][e] = f[q][e] * cs[q][e] + row[src[q][e]] * sn[q][e];
+    }
+  };
+
+  int64_t w_at = (int64_t)hl * a.chunks * 8 + at0;
+  for (int i0 = 0; i0 < rows;) {
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+      if (i0 + i >= rows) break;
+      const bool in = i0 + i + 1 < rows || last_in;
+      float f[2][8];
+      raw[i][0].get(f[0]);
+      raw[i][1].get(f[1]);
+      if constexpr (NORM == VC_NORM_HEAD) {
+        const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
+        inv = rsqrtf(fmaf(lanes_sum((ch0 ? q0 : 0.f) + (ch1 ? q1 : 0.f), lanes), a.inv_count[t], a.eps));
+      }
+      if constexpr (NORM != VC_NORM_NONE) {
+        times(f[0], inv);
+        times(f[1], inv);
+      }
+      if constexpr (NORM == VC_NORM_HEAD) {
+        times(f[0], wt[0]);
+        times(f[1], wt[1]);
+      }
+      if constexpr (NORM == VC_NORM_TOKEN) {
+        if (w && in) {
+          times_weights<T>(f[0], a, w, w_at);
+          times_weights<T>(f[1], a, w, w_at + step);
+        }
+        w_at += (int64_t)a.chunks * 8 << a.log_hl;
+      }
+      rotate(f);
+      if (in) {
+        if (live0) store8<T>(y, f[0]);
+        if (live1) store8<T>(y + step, f[1]);
+      }
+      y += sy;
+    }
+    i0 += kKeep;
+    if (i0 < rows) load_rows(i0);
   }
 }
 
@@ -459,10 +449,7 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
   while ((1 << a.log_hl) < rows && ((p->norm == VC_NORM_TOKEN && heads > keep << a.log_hl) || (heads >= 2 << a.log_hl && ctas() < 4 * sm_count()) ||
                                     (rows >> a.log_hl) >= 2 * p->N))
     ++a.log_hl;
-  // Several groups of tokens a CTA where that leaves every SM its share: addresses and angles are formed for all of them at once.
-  a.turns_taken = 1;
-  while (a.turns_taken < 8 && ctas() >= 16 * a.turns_taken * sm_count() && (2 * a.turns_taken * (rows >> a.log_hl)) * a.pairs <= 1024) a.turns_taken *= 2;
-  const int tokens = (rows >> a.log_hl) * a.turns_taken, tiles = (p->N + tokens - 1) / tokens;
+  const int tokens = rows >> a.log_hl, tiles = (p->N + tokens - 1) / tokens;
   const dim3 grid((unsigned)tiles, (unsigned)p->B, (unsigned)tensors);
   const size_t smem = rot == VC_ROTARY_NONE ? 0 : (size_t)tokens * a.pairs * sizeof(float2);
   cudaStream_t s = (cudaStream_t)stream;
