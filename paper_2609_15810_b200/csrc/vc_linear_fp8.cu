@@ -351,7 +351,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
         else emit_rows<float, kCols>(y, tile, static_cast<float*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, false, lane);
       }
     }
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // the rows have left before the CTA may end
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");       // the rows have left shared memory before the CTA may end
   }
   tc_fence_before();
   __syncthreads();

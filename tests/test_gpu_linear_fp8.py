@@ -159,20 +159,25 @@ def test_same_answer_other_stream_and_captured(M):
 
 
 @pytest.mark.parametrize("M,N", [(3, 400), (40, 400), (300, 400), (2500, 2560)])
-def test_wait_that_runs_out_is_reported_and_leaves_the_library_usable(M, N):
-    x, xs, w, ws = (_dev(t) for t in _operands(M, N, 1024, 12))
+@pytest.mark.parametrize("K", [1024, 16384])
+def test_wait_that_runs_out_is_reported_and_leaves_the_library_usable(M, N, K):
+    """With a limit of one poll a wait gives up unless what it waits for is there already.  At a few blocks of K, all copied in front of
+    the first wait, that can be so for every wait: then the answer is the right one.  At 128 blocks some wait gives up."""
+    x, xs, w, ws = (_dev(t) for t in _operands(M, N, K, 12))
     want = _run(x, xs, w, ws, "bf16")
     out = torch.empty_like(want)
     p = vc.LinearParams.of(x, w, out)
     work = torch.empty(vc.vc_linear_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    code = vc.VC_OK
     try:
         vc.vc_test_set_wait_limit(1)
         vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)
-        with pytest.raises(vc.VcError) as e:
-            vc.vc_poll_status(work)
-        assert e.value.code == vc.VC_ERR_TIMEOUT
+        vc.vc_poll_status(work)
+    except vc.VcError as e:
+        code = e.code
     finally:
         vc.vc_test_set_wait_limit(0)
+    assert code == vc.VC_ERR_TIMEOUT or (K == 1024 and code == vc.VC_OK and torch.equal(out, want))
     vc.vc_poll_status(work)
     vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)
     vc.vc_poll_status(work)
