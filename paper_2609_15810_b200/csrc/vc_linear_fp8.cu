@@ -241,20 +241,22 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     // An item's scales (of one block of K) and biases, fetched ahead: while the block in front is added, or the item in front written.
     // xa: of my row, or (SWAP) of row `lane` of my columns, xb of row 32 + lane; bias: of my columns lane, 32 + lane, ..., or (SWAP) of my row.
     float xa = 0.f, xb = 0.f, wv = 0.f, bias[kBias] = {};
-    auto fetch = [&](const Item& w, int kb) {
-      const float* xp = a.xs + (int64_t)kb * a.M;
-      if constexpr (SWAP) {
-        const int m = w.b0 + lane;
-        xa = lane < kCols && m < a.M ? __ldg(xp + m) : 0.f;
-        if constexpr (kCols > 32) xb = m + 32 < a.M ? __ldg(xp + m + 32) : 0.f;
-      } else {
-        xa = w.a0 + row < a.M ? __ldg(xp + w.a0 + row) : 0.f;
-      }
-      const int n0 = SWAP ? w.a0 : w.b0 + group * kCols;       // my (first) weight row; all of mine lie in its block of 128
-      wv = __ldg(a.ws + (int64_t)min(n0 >> 7, (a.N - 1) >> 7) * a.blocks + kb);
+    int xb_at = 0;
+    const float *xp = a.xs, *wp = a.ws;                        // where the next block's are (of a row outside: any, never stored)
+    auto fetch = [&] {
+      if (!SWAP || lane < kCols) xa = __ldg(xp);
+      if constexpr (SWAP && kCols > 32) xb = __ldg(xp + xb_at);
+      wv = __ldg(wp);
+      xp += a.M;
+      ++wp;
     };
     auto fetch_item = [&](const Item& w) {
-      fetch(w, w.kb0);
+      const int m = SWAP ? w.b0 + lane : w.a0 + row;
+      const int n0 = SWAP ? w.a0 : w.b0 + group * kCols;       // my (first) weight row; all of mine lie in its block of 128
+      xp = a.xs + (int64_t)w.kb0 * a.M + min(m, a.M - 1);
+      xb_at = min(m + 32, a.M - 1) - min(m, a.M - 1);
+      wp = a.ws + (int64_t)min(n0 >> 7, (a.N - 1) >> 7) * a.blocks + w.kb0;
+      fetch();
       if (whole && a.bias) {
 #pragma unroll
         for (int i = 0; i < kBias; ++i) {
@@ -275,7 +277,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
       for (int kb = w.kb0; kb < w.kb1; ++kb, ++n) {
         const int buf = n % C::kBufs;
         const float fa = xa * wv, fb = xb * wv;
-        if (kb + 1 < w.kb1) fetch(w, kb + 1);
+        if (kb + 1 < w.kb1) fetch();
         if (!(ok = wait(&sh->acc_full[buf], (n / C::kBufs) & 1, sh, a, 20))) break;
         tc_fence_after();
         const uint32_t at = lane_base + buf * TN;
