@@ -270,9 +270,9 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     Item w = item_of<TN>(a, blockIdx.x);
     fetch_item(w);
     for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
-      uint64_t acc[kCols / 2];
+      float y[kCols];
 #pragma unroll
-      for (int i = 0; i < kCols / 2; ++i) acc[i] = 0;
+      for (int i = 0; i < kCols; ++i) y[i] = 0.f;
       const int m0 = SWAP ? w.b0 : w.a0 + row, n0 = SWAP ? w.a0 : w.b0 + group * kCols;
       for (int kb = w.kb0; kb < w.kb1; ++kb, ++n) {
         const int buf = n % C::kBufs;
@@ -297,22 +297,14 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
             mbar_arrive(&sh->acc_free[buf]);
           }
 #pragma unroll
-          for (int i = 0; i < kChunk / 2; ++i) {
-            uint64_t f2;
-            if constexpr (SWAP) {
-              const float f = c == 0 ? fa : fb;
-              f2 = pack_f32x2(__shfl_sync(0xffffffffu, f, 2 * i), __shfl_sync(0xffffffffu, f, 2 * i + 1));
-            } else {
-              f2 = pack_f32x2(fa, fa);
-            }
-            acc[c * kChunk / 2 + i] = fma2(pack_b32x2(r[c & 1][2 * i], r[c & 1][2 * i + 1]), f2, acc[c * kChunk / 2 + i]);
+          for (int i = 0; i < kChunk; ++i) {
+            float f = fa;
+            if constexpr (SWAP) f = __shfl_sync(0xffffffffu, c == 0 ? fa : fb, i);
+            y[c * kChunk + i] = fmaf(__uint_as_float(r[c & 1][i]), f, y[c * kChunk + i]);
           }
         }
       }
       if (!ok) break;
-      float y[kCols];
-#pragma unroll
-      for (int i = 0; i < kCols / 2; ++i) unpack2(acc[i], y[2 * i], y[2 * i + 1]);
       float mine[kBias];
 #pragma unroll
       for (int i = 0; i < kBias; ++i) mine[i] = bias[i];
