@@ -413,6 +413,7 @@ vc_status resolve(const vc_linear_params* p, vc_linear_params* out, Plan* plan) 
   pl.items = tiles * pl.splits;
   if (pl.items > INT32_MAX) return VC_ERR_UNSUPPORTED;
   pl.ldp = (r.N + 3) / 4 * 4ll;
+  if (pl.splits > 1 && r.M * pl.ldp > 1ll << 40) return VC_ERR_UNSUPPORTED;      // (the parts' bytes stay far below 2^64)
   pl.total = 256 + (pl.splits > 1 ? (size_t)pl.splits * r.M * pl.ldp * 4 : 0);
   *out = r;
   *plan = pl;

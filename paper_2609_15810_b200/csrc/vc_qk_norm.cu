@@ -76,7 +76,7 @@ template <typename T> __device__ __forceinline__ void times_weights(float (&f)[8
 template <typename T, int NORM, int ROT>
 __global__ void __launch_bounds__(kThreads, 4)
 qk_norm_kernel(const __grid_constant__ QkArgs a) {
-  extern __shared__ float2 tab[];                       // [tokens of the CTA][pairs]
+  extern __shared__ __align__(16) float2 tab[];         // [tokens of the CTA][pairs]
   __shared__ float xch[ROT == VC_ROTARY_HALF ? kThreads * 16 + 1 : 1];  // (the last one is 0)
   __shared__ float part[NORM == VC_NORM_TOKEN ? kThreads / 32 : 1];
   constexpr int kKeep = heads_held(sizeof(T), ROT);
