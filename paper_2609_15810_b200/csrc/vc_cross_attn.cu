@@ -64,7 +64,8 @@ struct Smem {
 struct Item {
   int b, h, q0, split, t0, nt, len;
   bool two;
-  __device__ __forceinline__ bool has(int t, bool halves) const { return halves ? nt > t : t == 0 || two; }      // query tile t (half t of the keys)
+  // Is there work for query tile t (half t of the keys, with g key tiles of the CTA's in front of the item)?
+  __device__ __forceinline__ bool has(int t, bool halves, int g) const { return halves ? nt > (t ^ (g & 1)) : t == 0 || two; }
 };
 
 __device__ __forceinline__ Item item_of(const CrossArgs& a, int idx) {
@@ -122,7 +123,9 @@ template <int D> struct Lay {
   static constexpr uint32_t kO = 256, kOStride = D;
 };
 
-// HALVES: one query tile an item; its even and its odd key tiles take the places of two query tiles, and the epilogue joins them.
+// HALVES: one query tile an item; the CTA's even and its odd key tiles take the places of two query tiles, and the epilogue joins an
+// item's.  (Counted over all items of the CTA: a half that passed over key tiles would wait for a barrier's phase two ahead of
+// it, which reads as complete.)
 template <typename T, int D, bool HALVES>
 __global__ void __launch_bounds__(kThreads, 1)
 cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -198,7 +201,8 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           __syncwarp();
           fill(&tm_k, row, hk * a.k_h, w.b * a.k_b);
           if (j == 0) {                             // queries, each tile's when its predecessor's last scores are complete
-            for (int t = 0; t < 2 && w.has(t, HALVES); ++t) {
+            for (int t = 0; t < 2; ++t) {
+              if (!w.has(t, HALVES, g)) continue;
               if (!(ok = wait(&sh->q_free[t], (n[t] & 1) ^ 1, sh, a, 3))) break;
               if (elect_one()) {
                 mbar_expect_tx(&sh->q_full[t], L::kTile);
@@ -279,35 +283,36 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         return from;
       };
-      int idx = next_item(blockIdx.x, w);
+      int idx;
       if constexpr (HALVES) {
         // My key tiles one by one, and no turns: a tile's keys and values have one reader.
-        g = t;
-        auto skip = [&] {                           // items that have none for me
-          for (; idx < a.items && w.nt <= t; idx = next_item(idx + gridDim.x, w)) g += w.nt;
+        int before = 0, j0 = t;                     // key tiles in front of the item, its first one of mine
+        auto find = [&](int from) {                 // the next item that has one
+          for (idx = next_item(from, w); idx < a.items && w.nt <= (j0 = t ^ (before & 1)); idx = next_item(idx + gridDim.x, w)) before += w.nt;
+          g = before + j0;
         };
-        skip();
-        if (idx < a.items) scores(true, w.nt <= t + 2, true);
-        for (int j = t; ok && idx < a.items;) {
+        find(blockIdx.x);
+        if (idx < a.items) scores(true, w.nt <= j0 + 2, true);
+        for (int j = j0; ok && idx < a.items;) {
           const bool end = j + 2 >= w.nt;
-          outputs(j == t, end, true);
+          outputs(j == j0, end, true);
           ++uses;
           if (!ok) break;
           if (end) {
             ++items;
-            g += w.nt - j + t;
-            idx = next_item(idx + gridDim.x, w);
-            skip();
-            j = t;
+            before += w.nt;
+            find(idx + gridDim.x);
+            j = j0;
           } else {
             g += 2;
             j += 2;
           }
-          if (idx < a.items) scores(j == t, j + 2 >= w.nt, true);
+          if (idx < a.items) scores(j == j0, j + 2 >= w.nt, true);
         }
       } else {
         // S(0), [P(0) V, S(1)], [P(1) V, S(2)], ... across items.  A turn for every key tile, also where this query tile is not there.
         auto here = [&](const Item& it) { return t == 0 || it.two; };
+        idx = next_item(blockIdx.x, w);
         if (idx < a.items) {
           if (!my_turn()) {
           } else if (++turns, here(w)) {
@@ -377,9 +382,9 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
       const Item w = item_of(a, idx);
       if (w.nt == 0) continue;
-      if (!w.has(t, HALVES)) { g += w.nt; continue; }
+      if (!w.has(t, HALVES, g)) { g += w.nt; continue; }
       float m = -INFINITY, l = 0.f;                 // reference (log2 domain) and row sum
-      const int step = HALVES ? 2 : 1, j0 = HALVES ? t : 0;
+      const int step = HALVES ? 2 : 1, j0 = HALVES ? t ^ (g & 1) : 0;
       for (int j = j0; j < w.nt; j += step) {
         if (!(ok = wait(&sh->s_full[t], uses & 1, sh, a, 30))) break;
         ++uses;
@@ -459,25 +464,28 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     using Out = attn::OutTile<64>;                  // rows leave in lines of 128 bytes
     const int quarter = warp & 3;
     const uint32_t tile = smem_u32(sOut) + quarter * 32 * Out::ROW;
-    int uses[2] = {0, 0};
+    int uses[2] = {0, 0}, g = 0;
     bool ok = true;
     for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
       const Item w = item_of(a, idx);
+      const int half = HALVES ? g & 1 : 0;              // the half that has the item's first key tile
+      g += w.nt;
 #pragma unroll 1
       for (int t = 0; t < (w.two ? 2 : 1); ++t) {       // (the halves of the keys are joined in one pass)
         const int row0 = (w.q0 + t) * 128 + quarter * 32, rows = min(32, a.Nq - row0);
         const bool both = HALVES && w.nt > 1;
+        const int u = HALVES ? half : t;
         float inv = 0.f, inv1 = 0.f, lse2 = -INFINITY;
         // my row of the outputs' [B * H][N_q], behind those of the splits in front of this one
         const int64_t line = ((int64_t)w.split * a.heads + w.b * a.H + w.h) * a.Nq + row0 + lane;
         if (w.nt > 0) {
-          if (!(ok = wait(&sh->o_full[t], uses[t] & 1, sh, a, 40)) || (both && !(ok = wait(&sh->o_full[1], uses[1] & 1, sh, a, 41)))) break;
-          float2 ml = sh->ml[uses[t] & 1][t][quarter * 32 + lane];
-          ++uses[t];
+          if (!(ok = wait(&sh->o_full[u], uses[u] & 1, sh, a, 40)) || (both && !(ok = wait(&sh->o_full[u ^ 1], uses[u ^ 1] & 1, sh, a, 41)))) break;
+          float2 ml = sh->ml[uses[u] & 1][u][quarter * 32 + lane];
+          ++uses[u];
           float f0 = 1.f, f1 = 0.f;
           if (both) {                                 // o = (2^(m0 - m) O_0 + 2^(m1 - m) O_1) / (2^(m0 - m) l0 + 2^(m1 - m) l1)
-            const float2 ml1 = sh->ml[uses[1] & 1][1][quarter * 32 + lane];
-            ++uses[1];
+            const float2 ml1 = sh->ml[uses[u ^ 1] & 1][u ^ 1][quarter * 32 + lane];
+            ++uses[u ^ 1];
             const float m = fmaxf(ml.x, ml1.x), ms = m == -INFINITY ? 0.f : m;
             f0 = ex2_approx(ml.x - ms);
             f1 = ex2_approx(ml1.x - ms);
@@ -489,7 +497,7 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           lse2 = ml.y == 0.f ? -INFINITY : ml.x + log2f(ml.y);
           tc_fence_after();
         }
-        const uint32_t o_col = lane_base + L::kO + L::kOStride * t;
+        const uint32_t o_col = lane_base + L::kO + L::kOStride * u, o_col1 = lane_base + L::kO + L::kOStride * (u ^ 1);
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {                            // 32 channels
           uint32_t r[32];
@@ -502,7 +510,7 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #pragma unroll
               for (int q = 0; q < 2; ++q) {
                 uint32_t r1[16];
-                tmem_ld16(o_col + L::kOStride + 32 * c + 16 * q, r1);
+                tmem_ld16(o_col1 + 32 * c + 16 * q, r1);
                 tmem_wait_ld();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) r[16 * q + i] = __float_as_uint(fmaf(__uint_as_float(r1[i]), inv1, __uint_as_float(r[16 * q + i])));
@@ -510,8 +518,8 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
             if (c == D / 32 - 1) {
               tc_fence_before();
-              mbar_arrive(&sh->o_free[t]);
-              if (both) mbar_arrive(&sh->o_free[1]);
+              mbar_arrive(&sh->o_free[u]);
+              if (both) mbar_arrive(&sh->o_free[u ^ 1]);
             }
           } else {
 #pragma unroll

@@ -98,6 +98,20 @@ def test_keys_split_between_ctas(splits, d):
     _check(q, k, v, o, lse, lens)
 
 
+@pytest.mark.parametrize("splits", [5, 6, 12])
+@pytest.mark.parametrize("Nq", [1, 200])
+def test_many_parts_of_keys(splits, Nq):
+    """Few heads, and more parts of their keys than SMs: several a CTA, of no, one, two and three key tiles."""
+    B, H, N = 4, 9, 1500
+    g = torch.Generator().manual_seed(splits + Nq)
+    q, k, v = _heads(B, H, Nq, 128, "bf16", g, scale=2.0), _heads(B, 3, N, 128, "bf16", g), _heads(B, 3, N, 128, "bf16", g)
+    lens = torch.tensor([1500, 700, 0, 1290], dtype=torch.int32, device="cuda")
+    o, lse = _call(q, k, v, key_splits=splits)
+    _check(q, k, v, o, lse)
+    o, lse = _call(q, k, v, lens, key_splits=splits)
+    _check(q, k, v, o, lse, lens)
+
+
 @pytest.mark.parametrize("lens", [[0, 1, 127, 128], [129, 0, 400, 256], [-5, 500, 399, 2], [0, 0, 0, 0]])
 @pytest.mark.parametrize("splits", [1, 2])
 def test_lengths_per_batch(lens, splits):
