@@ -98,6 +98,24 @@ def test_keys_split_between_ctas(splits, d):
     _check(q, k, v, o, lse, lens)
 
 
+@pytest.mark.parametrize("dt,d", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("H,Nq", [(16, 1), (40, 100), (40, 128)])
+def test_heads_of_one_query_tile(dt, d, H, Nq):
+    """More heads than SMs, a query tile each: several items a CTA, of no, one, an odd and an even number of key tiles."""
+    B, N = 16, 600
+    g = torch.Generator().manual_seed(H + Nq)
+    q, k, v = _heads(B, H, Nq, d, dt, g, True, 2.0), _heads(B, 8, N, d, dt, g, True), _heads(B, 8, N, d, dt, g, True)
+    lens = torch.tensor([600, 0, 128, 1, 129, 300, 600, 257, 0, 0, 513, 384, 127, 130, 600, 256], dtype=torch.int32, device="cuda")
+    mask = torch.rand(B, N, generator=g) < 0.7
+    mask[3] = mask[6, :128] = mask[11, 128:256] = False
+    o, lse = _call(q, k, v)
+    _check(q, k, v, o, lse)
+    o, lse = _call(q, k, v, lens)
+    _check(q, k, v, o, lse, lens)
+    o, lse = _call(q, k, v, lens, mask.cuda())
+    _check(q, k, v, o, lse, lens, mask.cuda())
+
+
 @pytest.mark.parametrize("splits", [5, 6, 12])
 @pytest.mark.parametrize("Nq", [1, 200])
 def test_many_parts_of_keys(splits, Nq):
