@@ -4,13 +4,21 @@
 //
 // The scales are arbitrary FP32 numbers and differ from block to block of the common width, so no accumulator can run over
 // blocks: each S_kb is a product of its own (4 instructions of 32 columns into a tensor-memory buffer) and two
-// warpgroups add it, scaled, to sums in registers, 128 columns of a row a thread at most.  Per block and 128 x 256 tile
-// the products take 512 cycles, reading the buffer 256 (512 bytes a cycle) and the additions 256 of the FMA pipe, all three
-// side by side.
+// warpgroups add it, scaled, to sums in registers, 128 columns of a row a thread at most.
 //
-// Rows to A, weights to B (128 x 256 or 128 x 128), or the other way round where there are few rows: then 128 weight
-// rows are A, 16 or 64 rows of x are B, and the launch is bound by reading the weights.  With fewer tiles than SMs the blocks of K are
-// split between CTAs and the parts joined by a second launch in a fixed order.
+// Three shapes: tiles of 256 x 256 by two CTAs of a cluster (each 128 rows of A and half of B in shared memory, 128 rows of sums), where
+// these fill the SMs; tiles of 128 x 128; and up to 64 rows of x as B with 128 weight rows as A, which is bound by reading the weights.  With
+// fewer tiles than SMs the blocks of K are split between CTAs and the parts joined by a second launch in a fixed order.
+//
+// What bounds the large ones: per block the tensor cores need 512 cycles, 128 x 256 sums out of tensor memory 256 and their additions
+// 256 of the FMA pipe, side by side; but there are two buffers only (256 columns each of 512), and a buffer's round, product 512, signal 100,
+// read and additions 450, signal 150, takes longer than two products.  32760 x 5120 x 5120 745 us in single calls at 1965 MHz, 845 one
+// behind the other under the power cap (1500 MHz).  A CTA by itself on 128 x 256 (48 KB copied and 48 KB read per block and 512 cycles
+// from a shared memory that gives 128 bytes a cycle): 808 and 880.  One issuing warp instead of two that take every other block (a group of products
+// begins 150 cycles behind the end of the one in front if the same warp issued it): 781, and 845 under the cap.  A release or acquire of
+// cluster scope at the buffers' barriers: 1490 (it waits for every load in flight).  Packed additions: 860 (a move and a half each, the products
+// arrive in registers that do not pair up).  Four warpgroups of 64 columns, scales four blocks ahead: no gain.
+// One row 5120 x 5120: 9.3 us, 26 MB of weights 4.0; 1024 rows 58 us.
 #include "vc_attn_shared.cuh"
 #include "vc_layer.cuh"
 #include "vc_sm100.cuh"
@@ -38,18 +46,20 @@ struct LinearArgs {
 };
 
 // SWAP: A = weights (128 rows), B = TN rows of x.  Else A = 128 rows of x, B = TN weights.
+// TN 256: two CTAs of a cluster work on a tile of 256 x 256, each with 128 rows of A and, in shared memory, half of B.
 template <bool SWAP, int TN> struct Cfg {
+  static constexpr bool kPair = TN == 256;
   static constexpr int kGroups = TN >= 128 ? 2 : 1;            // warpgroups that add
   static constexpr int kCols = TN / kGroups;                   // columns of a thread
   static constexpr int kBufs = TN == 256 ? 2 : 4;
   static constexpr int kTmem = kBufs * TN;                     // 512, 512, 256, 64
-  static constexpr uint32_t kA = 128 * 128, kB = TN * 128, kStage = kA + kB;
-  static constexpr int kStages = TN == 256 ? 4 : TN == 128 ? 6 : 8;
+  static constexpr uint32_t kA = 128 * 128, kB = (kPair ? TN / 2 : TN) * 128, kStage = kA + kB;
+  static constexpr int kStages = TN >= 128 ? 6 : 8;
   static constexpr uint32_t kOut = SWAP ? 0 : 8 * 32 * 128;    // 128 bytes of each warp's 32 rows
 };
 
 template <int STAGES, int BUFS> struct Smem {
-  uint64_t full[STAGES], empty[STAGES], acc_full[BUFS], acc_free[BUFS], drain;
+  uint64_t full[STAGES], empty[STAGES], acc_full[BUFS], acc_free[BUFS], drain[2];
   uint32_t tmem_base;
   volatile int abort;
 };
@@ -74,12 +84,42 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, uin
                : "memory");
 }
 
-struct Item { int a0, b0, split, kb0, kb1; };                  // first rows of the tile in A and B; blocks of K
-template <int TN> __device__ __forceinline__ Item item_of(const LinearArgs& a, int idx) {
+// A pair of CTAs: the copy counts at a barrier of the leader's (`bar` is an address in the cluster), the product reads both
+// CTAs' shared memory and writes both CTAs' tensor memory, and its completion counts at the barrier of both.
+__device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m, uint32_t bar, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+               "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1)
+               : "memory");
+}
+__device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+               "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+               : "memory");
+}
+__device__ __forceinline__ void mma_commit_leader(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ uint32_t in_leader(const void* p) {       // the address of the leader's copy of `p`
+  uint32_t at;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_u32(p)));
+  return at;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
+struct Item { int a0, b0, split, kb0, kb1; };                  // first rows in A (this CTA's) and B (the tile's); blocks of K
+template <int TN> __device__ __forceinline__ Item item_of(const LinearArgs& a, int idx, int rank) {
   Item w;
   const int tile = idx / a.splits, ta = tile / a.tiles_b;
   w.split = idx - tile * a.splits;
-  w.a0 = ta * 128;
+  w.a0 = TN == 256 ? ta * 256 + rank * 128 : ta * 128;
   w.b0 = (tile - ta * a.tiles_b) * TN;
   w.kb0 = (int)((int64_t)a.blocks * w.split / a.splits);
   w.kb1 = (int)((int64_t)a.blocks * (w.split + 1) / a.splits);
@@ -166,20 +206,29 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
   unsigned char* sOut = smem + C::kStages * C::kStage;
   S* sh = reinterpret_cast<S*>(sOut + C::kOut);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = C::kPair ? blockIdx.x & 1 : 0, first = C::kPair ? blockIdx.x >> 1 : blockIdx.x, stride = C::kPair ? gridDim.x >> 1 : gridDim.x;
   if (tid == 0) {
     for (int i = 0; i < C::kStages; ++i) { mbar_init(&sh->full[i], 1); mbar_init(&sh->empty[i], 1); }
-    for (int i = 0; i < C::kBufs; ++i) { mbar_init(&sh->acc_full[i], 1); mbar_init(&sh->acc_free[i], 128 * C::kGroups); }
-    mbar_init(&sh->drain, 1);
+    for (int i = 0; i < C::kBufs; ++i) { mbar_init(&sh->acc_full[i], 1); mbar_init(&sh->acc_free[i], C::kPair ? 16 : 128 * C::kGroups); }
+    mbar_init(&sh->drain[0], 1); mbar_init(&sh->drain[1], 1);
     sh->abort = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tm_a); tma_prefetch_desc(&tm_b);
   }
   pdl_wait();
-  if (warp == 10) { tmem_alloc<C::kTmem>(&sh->tmem_base); tmem_relinquish(); }
+  if (warp == 10) {
+    if constexpr (C::kPair) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "n"(C::kTmem) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      tmem_alloc<C::kTmem>(&sh->tmem_base);
+      tmem_relinquish();
+    }
+  }
   if (tid == 0 && blockIdx.x == 0) *a.status = 0;
   if (a.splits > 1) pdl_allow();               // (what follows then is the launch that joins the parts: it may stand by)
   tc_fence_before();
-  __syncthreads();
+  if constexpr (C::kPair) cluster_sync(); else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh->tmem_base;
 
@@ -189,46 +238,71 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
       // -------------------------------------------------------------------------------- loads
       int n = 0;
       bool ok = true;
-      for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
-        const Item w = item_of<TN>(a, idx);
+      const uint32_t full = in_leader(&sh->full[0]);
+      for (int idx = first; ok && idx < a.items; idx += stride) {
+        const Item w = item_of<TN>(a, idx, rank);
         for (int kb = w.kb0; kb < w.kb1; ++kb, ++n) {
           const int st = n % C::kStages;
           if (!(ok = wait(&sh->empty[st], ((n / C::kStages) & 1) ^ 1, sh, a, 1))) break;
           if (elect_one()) {
             unsigned char* base = smem + st * C::kStage;
-            mbar_expect_tx(&sh->full[st], C::kStage);
-            tma_load_2d(base, &tm_a, &sh->full[st], kb * 128, w.a0);
-            tma_load_2d(base + C::kA, &tm_b, &sh->full[st], kb * 128, w.b0);
+            if constexpr (C::kPair) {
+              if (rank == 0) mbar_expect_tx(&sh->full[st], 2 * C::kStage);
+              tma_load_2d_pair(base, &tm_a, full + 8 * st, kb * 128, w.a0);
+              tma_load_2d_pair(base + C::kA, &tm_b, full + 8 * st, kb * 128, w.b0 + 128 * rank);
+            } else {
+              mbar_expect_tx(&sh->full[st], C::kStage);
+              tma_load_2d(base, &tm_a, &sh->full[st], kb * 128, w.a0);
+              tma_load_2d(base + C::kA, &tm_b, &sh->full[st], kb * 128, w.b0);
+            }
           }
           __syncwarp();
         }
       }
-      // every copy issued has landed before the CTA may end (at once on a normal run)
+      // Every copy issued has landed before the CTA may end (at once on a normal run).  A pair's land at the leader's barriers: what
+      // says so in both is that they have been read; where a wait has given up, time.
+      if constexpr (C::kPair) {
+        for (int i = n > C::kStages ? n - C::kStages : 0; ok && i < n; ++i) ok = wait(&sh->empty[i % C::kStages], (i / C::kStages) & 1, sh, a, 2);
+        if (!ok)
+          for (int i = 0; i < 10; ++i) __nanosleep(20000);
+      } else
       for (int i = n > C::kStages ? n - C::kStages : 0; i < n; ++i) mbar_wait(&sh->full[i % C::kStages], (i / C::kStages) & 1, attn::kDrainLimit);
-    } else if (warp == 9) {
-      // -------------------------------------------------------------------------------- products
-      constexpr uint32_t idesc = idesc_e4m3(128, TN);
+    } else if ((warp == 9 || warp == 11) && rank == 0) {
+      // -------------------------------------------------------------------------------- products: two warps, every other block each
+      const int mine = warp >> 1 & 1;
+      constexpr uint32_t idesc = idesc_e4m3(C::kPair ? 256 : 128, TN);
       int n = 0;
       bool ok = true;
-      for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
-        const Item w = item_of<TN>(a, idx);
+      for (int idx = first; ok && idx < a.items; idx += stride) {
+        const Item w = item_of<TN>(a, idx, rank);
         for (int kb = w.kb0; kb < w.kb1; ++kb, ++n) {
+          if ((n & 1) != mine) continue;             // (stages and buffers are even in number: each has one of the warps)
           const int st = n % C::kStages, buf = n % C::kBufs;
           if (!(ok = wait(&sh->full[st], (n / C::kStages) & 1, sh, a, 10)) || !(ok = wait(&sh->acc_free[buf], ((n / C::kBufs) & 1) ^ 1, sh, a, 11))) break;
           if (elect_one()) {
             tc_fence_after();
             const uint64_t da = smem_desc_kmajor(smem_u32(smem + st * C::kStage), 128), db = smem_desc_kmajor(smem_u32(smem + st * C::kStage + C::kA), 128);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mma_f8_ss(tmem + buf * TN, da + 2 * k, db + 2 * k, idesc, k > 0);
-            mma_commit(&sh->empty[st]);
-            mma_commit(&sh->acc_full[buf]);
+            for (int k = 0; k < 4; ++k) {
+              if constexpr (C::kPair) mma_f8_pair(tmem + buf * TN, da + 2 * k, db + 2 * k, idesc, k > 0);
+              else mma_f8_ss(tmem + buf * TN, da + 2 * k, db + 2 * k, idesc, k > 0);
+            }
+            if constexpr (C::kPair) {
+              mma_commit_pair(&sh->empty[st]);
+              mma_commit_pair(&sh->acc_full[buf]);
+            } else {
+              mma_commit(&sh->empty[st]);
+              mma_commit(&sh->acc_full[buf]);
+            }
           }
           __syncwarp();
         }
       }
-      if (elect_one()) mma_commit(&sh->drain);
+      if (elect_one()) {
+        if constexpr (C::kPair) mma_commit_leader(&sh->drain[mine]); else mma_commit(&sh->drain[mine]);
+      }
       __syncwarp();
-      mbar_wait(&sh->drain, 0, attn::kDrainLimit);
+      mbar_wait(&sh->drain[mine], 0, attn::kDrainLimit);
     }
   } else if (warp < 4 * C::kGroups) {
     // ---------------------------------------------------------------------------------- sums
@@ -267,9 +341,10 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     };
     int n = 0;
     bool ok = true;
-    Item w = item_of<TN>(a, blockIdx.x);
+    const uint32_t acc_free = in_leader(&sh->acc_free[0]);
+    Item w = item_of<TN>(a, first, rank);
     fetch_item(w);
-    for (int idx = blockIdx.x; ok && idx < a.items; idx += gridDim.x) {
+    for (int idx = first; ok && idx < a.items; idx += stride) {
       float y[kCols];
 #pragma unroll
       for (int i = 0; i < kCols; ++i) y[i] = 0.f;
@@ -294,7 +369,12 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
             load(c + 1);
           } else {
             tc_fence_before();
-            mbar_arrive(&sh->acc_free[buf]);
+            if constexpr (C::kPair) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cluster(acc_free + 8 * buf);
+            } else {
+              mbar_arrive(&sh->acc_free[buf]);
+            }
           }
 #pragma unroll
           for (int i = 0; i < kChunk; ++i) {
@@ -309,8 +389,8 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
 #pragma unroll
       for (int i = 0; i < kBias; ++i) mine[i] = bias[i];
       const Item now = w;
-      if (idx + (int)gridDim.x < a.items) {
-        w = item_of<TN>(a, idx + gridDim.x);
+      if (idx + stride < a.items) {
+        w = item_of<TN>(a, idx + stride, rank);
         fetch_item(w);
       }
       if constexpr (SWAP) {
@@ -348,8 +428,13 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");       // the rows have left shared memory before the CTA may end
   }
   tc_fence_before();
-  __syncthreads();
-  if (warp == 10) tmem_dealloc<C::kTmem>(tmem);
+  if constexpr (C::kPair) {
+    cluster_sync();                            // (neither CTA ends, nor gives its tensor memory back, while the other's products or signals reach it)
+    if (warp == 10) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(C::kTmem) : "memory");
+  } else {
+    __syncthreads();
+    if (warp == 10) tmem_dealloc<C::kTmem>(tmem);
+  }
 }
 
 // The parts of every sum in the order of the splits, the bias, the rounding.  A thread takes four columns of a row.
@@ -397,14 +482,14 @@ vc_status resolve(const vc_linear_params* p, vc_linear_params* out, Plan* plan) 
   pl.blocks = (r.K + 127) / 128;
   // Up to 64 rows: weights are A.  Else the wide tile where it fills the SMs, the narrow one where that has more tiles to give.
   pl.swap = r.M <= 64;
-  const int64_t ta = pl.swap ? (r.N + 127) / 128 : (r.M + 127) / 128;
   if (pl.swap) pl.tn = r.M <= 16 ? 16 : 64;
-  else pl.tn = ta * ((r.N + 255) / 256) >= kSms ? 256 : 128;
+  else pl.tn = ((r.M + 255) / 256) * ((r.N + 255ll) / 256) >= kSms / 2 ? 256 : 128;
+  const int64_t ta = pl.swap ? (r.N + 127) / 128 : pl.tn == 256 ? (r.M + 255) / 256 : (r.M + 127) / 128;
   pl.tiles_b = (int)(((pl.swap ? r.M : r.N) + (int64_t)pl.tn - 1) / pl.tn);
-  const int64_t tiles = ta * pl.tiles_b;
+  const int64_t tiles = ta * pl.tiles_b, ctas = pl.tn == 256 ? 2 : 1;        // (of a tile)
   pl.splits = r.k_splits;
   if (pl.splits == 0) {
-    const int64_t room = kSms / tiles;
+    const int64_t room = kSms / (tiles * ctas);
     pl.splits = 1;
     if (room > 1 && pl.blocks >= 8) pl.splits = (int)(room < pl.blocks / 4 ? room : pl.blocks / 4);
   }
@@ -446,15 +531,16 @@ cudaError_t launch_linear(const vc_linear_params& r, const Plan& pl, const Linea
   using C = Cfg<SWAP, TN>;
   alignas(64) CUtensorMap ta, tb, to;
   if (!make_map8(&ta, SWAP ? w : x, SWAP ? r.N : r.M, r.K, SWAP ? r.ldw : r.ldx, 128) ||
-      !make_map8(&tb, SWAP ? x : w, SWAP ? r.M : r.N, r.K, SWAP ? r.ldx : r.ldw, TN))
+      !make_map8(&tb, SWAP ? x : w, SWAP ? r.M : r.N, r.K, SWAP ? r.ldx : r.ldw, C::kPair ? TN / 2 : TN))
     return cudaErrorUnknown;
   to = ta;                                   // (read where rows leave by copies alone)
   if (!SWAP && a.vec && pl.splits == 1 && !make_map_out(&to, a.out, r)) return cudaErrorUnknown;
   cudaError_t e = allow_smem<linear_fp8_kernel<SWAP, TN>>();
   if (e != cudaSuccess) return e;
-  const int grid = pl.items < sm_count() ? (int)pl.items : sm_count();
+  constexpr int kCtas = C::kPair ? 2 : 1;
+  const int room = sm_count() / kCtas, grid = kCtas * (pl.items < room ? (int)pl.items : room);
   constexpr size_t smem = C::kStages * C::kStage + C::kOut + sizeof(Smem<C::kStages, C::kBufs>);
-  e = launch_overlapped(linear_fp8_kernel<SWAP, TN>, dim3((unsigned)grid), kThreads, smem, s, ta, tb, to, a);
+  e = launch_clusters(linear_fp8_kernel<SWAP, TN>, dim3((unsigned)grid), kCtas, kThreads, smem, s, ta, tb, to, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
   if (pl.splits > 1) {

@@ -84,6 +84,14 @@ def test_wide_tiles(N):
     _check(2500, N, 144, "fp32", bias_dt="fp16")
 
 
+@pytest.mark.parametrize("M,N", [(2305, 2560), (2433, 2600), (256 * 75, 130), (100, 256 * 80)])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_tiles_of_two_ctas(M, N, splits):
+    """A CTA without rows, halves of weights that end inside or in front of a tile, one tile and more a pair, sums split between pairs."""
+    _check(M, N, 640, "bf16", k_splits=splits)
+    _check(M, N, 16, "fp16", bias=False, k_splits=splits)
+
+
 @pytest.mark.parametrize("M", [5, 50, 200, 2500])
 def test_rows_of_wider_matrices_and_neighbours(M):
     N, K = 2500, 160
