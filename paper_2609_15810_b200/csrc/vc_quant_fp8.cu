@@ -3,6 +3,9 @@
 // Bound by memory: two or four bytes in, one out.  block_rows 1: eight lanes hold the 128 columns of a row's block, sixteen
 // each, so the codes leave 16 bytes at a time and the maximum is three shuffles; a CTA takes 32 rows, whose scales
 // lie side by side.  block_rows 128: a CTA holds its block in registers between the maximum and the codes.
+//
+// 40 heads x 32760 x 128 in bf16 (508 MB): 89 us, 88 % of the measured copy rate; the issue slots are 67 % taken, the ALU half.  One block of
+// columns in flight a thread or four, CTAs of 128 or 512 threads: no better over the sizes.
 #include <cuda_fp8.h>
 
 #include "vc_layer.cuh"
