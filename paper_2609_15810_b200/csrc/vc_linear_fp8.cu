@@ -62,6 +62,7 @@ template <int STAGES, int BUFS> struct Smem {
   uint64_t full[STAGES], empty[STAGES], acc_full[BUFS], acc_free[BUFS], drain[2];
   uint32_t tmem_base;
   volatile int abort;
+  float touched[32];                         // (never read)
 };
 
 template <class S>
@@ -257,8 +258,14 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
             }
           }
           __syncwarp();
+          // The block's scales into the first-level cache: the adding warps fetch them one block ahead, less than the latency of L2
+          // (257 x 5120 x 13824 48.5 -> 35.9 us, 8192 x 5120 x 5120 196 -> 187; two or four blocks ahead into registers: 37, and others +5 %).
+          const float* scale = lane < 17 ? a.xs + (int64_t)kb * a.M + min((SWAP ? w.b0 : w.a0) + min(8 * lane, SWAP ? TN - 1 : 127), a.M - 1)
+                                         : a.ws + (int64_t)min(((SWAP ? w.a0 : w.b0) >> 7) + (lane & 1), (a.N - 1) >> 7) * a.blocks + kb;
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(&sh->touched[lane])), "l"(scale) : "memory");
         }
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
       // Every copy issued has landed before the CTA may end (at once on a normal run).  A pair's land at the leader's barriers: what
       // says so in both is that they have been read; where a wait has given up, time.
       if constexpr (C::kPair) {
@@ -480,10 +487,14 @@ vc_status resolve(const vc_linear_params* p, vc_linear_params* out, Plan* plan) 
   if (r.ldx < r.K || r.ldw < r.K || r.ldo < r.N || r.ldx % 16 || r.ldw % 16 || r.ldx >= 1ll << 38 || r.ldw >= 1ll << 38 || r.ldo >= 1ll << 32) return VC_ERR_INVALID_ARG;
   Plan pl{};
   pl.blocks = (r.K + 127) / 128;
-  // Up to 64 rows: weights are A.  Else the wide tile where it fills the SMs, the narrow one where that has more tiles to give.
+  // Up to 64 rows: weights are A.  Else a pair of CTAs takes 0.53 us for a block of 256 x 256, a CTA 0.33 for one of 128 x 128: the shape whose
+  // rounds over the SMs cost less (512 x 5120 x 5120: 40 tiles of a pair 22.2 us, 160 of a CTA 26.8; 257 x 13824 x 5120: 49.0, 41.1).
   pl.swap = r.M <= 64;
   if (pl.swap) pl.tn = r.M <= 16 ? 16 : 64;
-  else pl.tn = ((r.M + 255) / 256) * ((r.N + 255ll) / 256) >= kSms / 2 ? 256 : 128;
+  else {
+    auto rounds = [&](int64_t t, int at_once) { return (((r.M + t - 1) / t) * ((r.N + t - 1) / t) + at_once - 1) / at_once; };
+    pl.tn = 8 * rounds(256, kSms / 2) <= 5 * rounds(128, kSms) ? 256 : 128;
+  }
   const int64_t ta = pl.swap ? (r.N + 127) / 128 : pl.tn == 256 ? (r.M + 255) / 256 : (r.M + 127) / 128;
   pl.tiles_b = (int)(((pl.swap ? r.M : r.N) + (int64_t)pl.tn - 1) / pl.tn);
   const int64_t tiles = ta * pl.tiles_b, ctas = pl.tn == 256 ? 2 : 1;        // (of a tile)
