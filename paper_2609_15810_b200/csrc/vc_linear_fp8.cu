@@ -12,10 +12,11 @@
 //
 // What bounds the large ones: per block the tensor cores need 512 cycles, 128 x 256 sums out of tensor memory 256 and their additions
 // 256 of the FMA pipe, side by side; but there are two buffers only (256 columns each of 512), and a buffer's round, product 512, signal 100,
-// read and additions 450, signal 150, takes longer than two products.  32760 x 5120 x 5120 745 us in single calls at 1965 MHz, 845 one
+// read and additions 450, signal 150, takes longer than two products.  32760 x 5120 x 5120 735 us in single calls at 1965 MHz, 805 one
 // behind the other under the power cap (1500 MHz).  A CTA by itself on 128 x 256 (48 KB copied and 48 KB read per block and 512 cycles
 // from a shared memory that gives 128 bytes a cycle): 808 and 880.  One issuing warp instead of two that take every other block (a group of products
-// begins 150 cycles behind the end of the one in front if the same warp issued it): 781, and 845 under the cap.  A release or acquire of
+// begins 150 cycles behind the end of the one in front if the same warp issued it): 781, and the same under the cap.  Four buffers of
+// 128 columns (two products of 256 x 128 a block, A read twice): 794, and 868 under the cap.  A release or acquire of
 // cluster scope at the buffers' barriers: 1490 (it waits for every load in flight).  Packed additions: 860 (a move and a half each, the products
 // arrive in registers that do not pair up).  Four warpgroups of 64 columns, scales four blocks ahead: no gain.
 // One row 5120 x 5120: 9.3 us, 26 MB of weights 4.0; 1024 rows 58 us.
