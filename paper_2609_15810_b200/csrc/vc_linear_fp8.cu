@@ -19,7 +19,7 @@
 // 128 columns (two products of 256 x 128 a block, A read twice): 794, and 868 under the cap.  A release or acquire of
 // cluster scope at the buffers' barriers: 1490 (it waits for every load in flight).  Packed additions: 860 (a move and a half each, the products
 // arrive in registers that do not pair up).  Four warpgroups of 64 columns, scales four blocks ahead: no gain.
-// One row 5120 x 5120: 9.3 us, 26 MB of weights 4.0; 1024 rows 58 us.
+// 5120 x 5120 with weights in L2: one row 8.1 us (two launches; 26 MB at the copy rate 4.0), 512 rows 22, 1024 rows 40.
 #include "vc_attn_shared.cuh"
 #include "vc_layer.cuh"
 #include "vc_sm100.cuh"

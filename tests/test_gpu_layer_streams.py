@@ -73,6 +73,48 @@ def test_two_streams_at_once(which, graphs):
             assert torch.equal(t, r)
 
 
+def _attention_call(seed):
+    g = torch.Generator().manual_seed(seed)
+    q, k, v = (torch.randn(1, 4, 1280, 128, generator=g).to(BF).cuda() for _ in range(3))
+    o = torch.empty_like(q)
+    p = Params.make(1, 4, 1280, 128, (10, 8, 16), flags=vc.VC_FLAG_ALL & ~vc.VC_FLAG_ROPE)
+    quant, work = alloc_buffers(p)
+    return (lambda: vc.vc_attn(p, q, k, v, None, o, quant, work)), (o,), work
+
+
+def _wide_linear_call(seed, M, N, K=1024):
+    g = torch.Generator().manual_seed(seed)
+    x, w = (torch.randint(0, 120, (n, K), generator=g, dtype=torch.uint8).cuda() for n in (M, N))
+    xs, ws = torch.rand(K // 128, M, generator=g).cuda(), torch.rand((N + 127) // 128, K // 128, generator=g).cuda()
+    out = torch.empty(M, N, dtype=BF, device="cuda")
+    p = vc.LinearParams.of(x, w, out)
+    work = torch.empty(vc.vc_linear_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    return (lambda: vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)), (out,), work
+
+
+def test_every_kind_at_once():
+    """Products by pairs of CTAs and by single ones, both attentions, on five streams: they take turns on the SMs and their tensor memory."""
+    calls = [_wide_linear_call(1, 5000, 2000), _wide_linear_call(2, 3000, 2560), _wide_linear_call(3, 700, 640), _cross_call(4, 2000, 700, H=12), _attention_call(5)]
+    for call, _, work in calls:
+        call()
+        vc.vc_poll_status(work)
+    want = [[t.clone() for t in outs] for _, outs, _ in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _, outs, _ in calls:
+        for t in outs:
+            t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(40):
+        for s, (call, _, _) in zip(streams, calls):
+            with torch.cuda.stream(s):
+                call()
+    torch.cuda.synchronize()
+    for (_, outs, work), ref in zip(calls, want):
+        vc.vc_poll_status(work)
+        for t, r in zip(outs, ref):
+            assert torch.equal(t, r)
+
+
 def test_one_tensor_as_queries_keys_and_values():
     g = torch.Generator().manual_seed(3)
     x = torch.randn(1, 2, 333, 64, generator=g).to(BF).cuda()
