@@ -353,7 +353,7 @@ typedef struct { int64_t b, h, n; } vc_strides;
  *                                                  over all heads of a token (VC_NORM_TOKEN, weight [H][d])
  *   (a, b) -> m (a cos t - b sin t, a sin t + b cos t)      t = position * frequency, for every pair (a, b) of channels
  *
- * computed in FP32 (the angle in FP64) and rounded once.  The rotated channels are the first
+ * computed in FP32 (the angle in 64 bits) and rounded once.  The rotated channels are the first
  * rope_dim_t + rope_dim_h + rope_dim_w of a head, in this order, one position axis each; the others
  * pass through.  Pair i of an axis with n channels from channel s on is (s + 2 i, s + 2 i + 1)
  * (VC_ROTARY_INTERLEAVED, what VC_FLAG_ROPE does) or (s + i, s + n / 2 + i) (VC_ROTARY_HALF), and its frequency is

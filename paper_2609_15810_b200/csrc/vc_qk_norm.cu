@@ -5,10 +5,11 @@
 // shared memory), loads and stores are 16 bytes, and a head's sum of squares is a shuffle within its lanes.  The norm over
 // a token keeps the thread's part of the token in registers between the sum and the rotation: one pass over memory.
 //
-// 40 + 40 heads x 32760 x 128, interleaved: rotation alone 215 us (96 % of the measured copy rate), with the norm per head 237, per token 260
-// (1342 MB; a CTA's loads stand still while a token's sum is formed, and 57 % of the issue slots are taken).  Eight channels a thread instead of
-// 16: 302 (angles, addresses and shuffles per row cost twice as much); CTAs of 256 threads: 282 (more warps wait for a token's slowest).
-// Halves with axes that are not multiples of 16 channels: 268 us for 24 + 24 heads (floor 124), the change of places in shared memory bounds it.
+// 32760 tokens of d128, interleaved, 40 + 40 / 12 + 12 heads: rotation alone 213 / 66 us (97 / 94 % of the measured copy rate), with the norm per head
+// 229 / 85, per token 253 / 92 (1342 / 403 MB; a CTA's loads stand still while a token's sum is formed, and the angles cost 14 to 19).  Eight
+// channels a thread instead of 16: 302 for 260 at that time (angles, addresses and shuffles per row cost twice as much); CTAs of 256 threads: 282 (more
+// warps wait for a token's slowest); five or six CTAs an SM: 284 and 326 (spills), with three heads a thread 12 heads 98 for 105, 40 heads 333.
+// Halves with axes that are not multiples of 16 channels: 263 us for 24 + 24 heads (floor 124), the change of places in shared memory bounds it.
 #include <cmath>
 
 #include "vc_layer.cuh"
@@ -31,6 +32,7 @@ struct QkArgs {
   const int32_t* positions;
   vc_strides in[2], out[2];
   int H[2], first;                 // first: 1 if there is no Q
+  bool both;                       // a CTA takes its tokens' Q, then their K (else blockIdx.z is one of them)
   int N, chunks, log_lanes, log_hl, log_pairs, weight_dtype;     // log_pairs: 2^log_pairs >= pairs
   bool same_type;                  // weights are of the tensors' type
   bool partial;                    // some channels are not rotated
@@ -38,29 +40,37 @@ struct QkArgs {
   uint8_t lo[16], hi[16], first_pair[16];
   int pairs, pair_end[3];          // rotated pairs; where each axis's pairs end
   int grid_h, grid_w, start[3];
+  float inv_w, inv_h;              // about 1 / grid_w, 1 / grid_h
   float eps, inv_count[2], mult;
-  double turns[kMaxPairs];         // frequency of a pair in turns per position
+  uint64_t turns[kMaxPairs];       // frequency of a pair in turns per position, 64 bits behind the point
 };
 
-// Angles of the CTA's tokens.  The product is formed in FP64: in FP32 the angle of position 10^5 is off by 10^-2.
-// Whole turns are taken off there too, and sincospi sees |x| <= 1.
+// n / by for n and by up to 2^22, inv about 1 / by: the quotient in FP32 is off by one at most.
+__device__ __forceinline__ int quotient(int n, int by, float inv) {
+  const int q = __float2int_rd((float)n * inv), r = n - q * by;
+  return q + (r >= by) - (r < 0);
+}
+
+// Angles of the CTA's tokens.  The product of position and frequency is formed in 64-bit fixed point, whose overflow takes off the whole
+// turns: its error is 2^-33 turns at most (in FP32 the angle of position 10^5 is off by 10^-2; in FP64, with the integer
+// divisions of the position, a table took twice as long: 12 + 12 heads x 32760 x 128, norm per head, 94.3 us instead of 85.2).
 __device__ __forceinline__ void fill_table(const QkArgs& a, float2* tab, int b, int n0, int tokens) {
   const int p = threadIdx.x & ((1 << a.log_pairs) - 1);
   if (p >= a.pairs) return;
   const int axis = (p >= a.pair_end[0]) + (p >= a.pair_end[1]);
-  const double turns = a.turns[p];
+  const uint64_t turns = a.turns[p];
   for (int tt = threadIdx.x >> a.log_pairs; tt < tokens; tt += kThreads >> a.log_pairs) {
     const int n = min(n0 + tt, a.N - 1);
     int pos;
     if (a.positions) {
       pos = a.positions[((int64_t)b * a.N + n) * 3 + axis];
     } else {
-      const int row = n / a.grid_w;
-      pos = a.start[axis] + (axis == 2 ? n - row * a.grid_w : axis == 1 ? row % a.grid_h : row / a.grid_h);
+      const int row = quotient(n, a.grid_w, a.inv_w), t = quotient(row, a.grid_h, a.inv_h);
+      pos = a.start[axis] + (axis == 2 ? n - row * a.grid_w : axis == 1 ? row - t * a.grid_h : t);
     }
-    const double t = (double)pos * turns;
+    const uint64_t t = (uint64_t)(int64_t)pos * turns;
     float s, c;
-    sincospif(2.0f * (float)(t - rint(t)), &s, &c);
+    sincospif((float)(int32_t)(t >> 32) * 0x1p-31f, &s, &c);      // half turns, in [-1, 1]
     tab[tt * a.pairs + p] = make_float2(c * a.mult, s * a.mult);
   }
 }
@@ -83,23 +93,24 @@ __global__ void __launch_bounds__(kThreads, 4)
 qk_norm_kernel(const __grid_constant__ QkArgs a) {
   extern __shared__ __align__(16) float2 tab[];         // [tokens of the CTA][pairs]
   __shared__ float xch[ROT == VC_ROTARY_HALF ? kThreads * 16 + 1 : 1];  // (the last one is 0)
-  __shared__ float part[NORM == VC_NORM_TOKEN ? kThreads / 32 : 1];
+  __shared__ float part[NORM == VC_NORM_TOKEN ? 2 : 1][kThreads / 32];
   constexpr int kKeep = heads_held(sizeof(T), ROT);
   const int lanes = 1 << a.log_lanes, tokens = kThreads >> (a.log_lanes + a.log_hl);
   const int c = threadIdx.x & (lanes - 1), r = threadIdx.x >> a.log_lanes, hl = r & ((1 << a.log_hl) - 1), tt = r >> a.log_hl;
   const int b = blockIdx.y, n0 = blockIdx.x * tokens, n = n0 + tt;
-  const int t = blockIdx.z + a.first, H = a.H[t];       // Q or K
-  const void* w = a.w[t];
-  // My channels: two groups of eight.  My heads: hl, hl + hls, ..., `rows` of them, the last one perhaps
-  // behind H.  (What lies outside reads another place and is neither summed nor stored.)
-  const int rows = (H + (1 << a.log_hl) - 1) >> a.log_hl;
+  const int first = a.both ? 0 : blockIdx.z + a.first, last = a.both ? 1 : first;       // Q, K or (the norm over a token alone) Q and then K
+  // My channels: two groups of eight.
   const int lo = a.lo[c], hi = a.hi[c];
-  const bool ch0 = lo != 255, ch1 = hi != 255, last_in = hl + ((rows - 1) << a.log_hl) < H;
-  const int64_t sx = a.in[t].h << a.log_hl, sy = a.out[t].h << a.log_hl;
-  const int at0 = 8 * (ch0 ? lo : 0), at1 = 8 * (ch1 ? hi : 0);
-  const T* x = static_cast<const T*>(a.x[t]) + (b * a.in[t].b + (hl < H ? hl : 0) * a.in[t].h + (int64_t)min(n, a.N - 1) * a.in[t].n + at0);
-  T* y = static_cast<T*>(a.y[t]) + (b * a.out[t].b + hl * a.out[t].h + (int64_t)n * a.out[t].n + at0);
-  const int step = at1 - at0;
+  const bool ch0 = lo != 255, ch1 = hi != 255;
+  const int at0 = 8 * (ch0 ? lo : 0), at1 = 8 * (ch1 ? hi : 0), step = at1 - at0;
+  const bool live0 = n < a.N && ch0, live1 = n < a.N && ch1;
+  // cos and sin of my channels.  One that is not rotated keeps its value whatever its neighbour holds: bit e of `still`, or 0 in the
+  // place of the other half (with as many bits to test the predicate registers run out).
+  constexpr int kAngles = ROT >= VC_ROTARY_HALF ? 8 : 4;
+  float cs[2][kAngles], sn[2][kAngles];
+  int src[2][ROT == VC_ROTARY_HALF ? 8 : 1];
+  uint32_t still = 0;
+  const bool turned = ROT == kRotaryWhole && a.first_pair[c] != 255;
 
   auto lanes_sum = [](float v, int count) {
     for (int s = count >> 1; s > 0; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
@@ -117,181 +128,194 @@ qk_norm_kernel(const __grid_constant__ QkArgs a) {
     sm100::unpack2(s, even, odd);
     return even + odd;
   };
-  pdl_wait();
-  Raw8<T> raw[kKeep][2];
-  auto load_rows = [&](int i0) {                        // heads i0, i0 + 1, ... of mine
-    const T* from = x + i0 * sx;
-#pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      if (i0 + i >= rows) break;
-      if (i0 + i + 1 == rows && !last_in) from = x;
-      raw[i][0].load(from);
-      raw[i][1].load(from + step);
-      from += sx;
-    }
-  };
-  load_rows(0);                                         // (on their way while the angles are formed)
-  float wt[2][8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) wt[0][e] = wt[1][e] = 1.f;
-  if (NORM == VC_NORM_HEAD && w) {
-    times_weights<T>(wt[0], a, w, at0);
-    times_weights<T>(wt[1], a, w, at1);
-  }
-  if constexpr (ROT != VC_ROTARY_NONE) fill_table(a, tab, b, n0, tokens);
-  if (ROT == VC_ROTARY_HALF && threadIdx.x == 0) xch[kThreads * 16] = 0.f;
-  if constexpr (ROT != VC_ROTARY_NONE && NORM != VC_NORM_TOKEN) __syncthreads();
-
-  const bool live0 = n < a.N && ch0, live1 = n < a.N && ch1;
-  float inv = 1.f;
-  if constexpr (NORM == VC_NORM_TOKEN) {
-    float ss0 = 0.f, ss1 = 0.f;
-    for (int i0 = 0;;) {
+  auto side = [&](const int t) {
+    const int H = a.H[t];
+    const void* w = a.w[t];
+    // My heads: hl, hl + hls, ..., `rows` of them, the last one perhaps behind H.  (What lies outside reads another place and is
+    // neither summed nor stored.)
+    const int rows = (H + (1 << a.log_hl) - 1) >> a.log_hl;
+    const bool last_in = hl + ((rows - 1) << a.log_hl) < H;
+    const int64_t sx = a.in[t].h << a.log_hl, sy = a.out[t].h << a.log_hl;
+    const T* x = static_cast<const T*>(a.x[t]) + (b * a.in[t].b + (hl < H ? hl : 0) * a.in[t].h + (int64_t)min(n, a.N - 1) * a.in[t].n + at0);
+    T* y = static_cast<T*>(a.y[t]) + (b * a.out[t].b + hl * a.out[t].h + (int64_t)n * a.out[t].n + at0);
+    if (t == first) pdl_wait();
+    Raw8<T> raw[kKeep][2];
+    auto load_rows = [&](int i0) {                        // heads i0, i0 + 1, ... of mine
+      const T* from = x + i0 * sx;
 #pragma unroll
       for (int i = 0; i < kKeep; ++i) {
         if (i0 + i >= rows) break;
-        const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
-        if (i0 + i + 1 < rows || last_in) { ss0 += q0; ss1 += q1; }
+        if (i0 + i + 1 == rows && !last_in) from = x;
+        raw[i][0].load(from);
+        raw[i][1].load(from + step);
+        from += sx;
       }
-      i0 += kKeep;
-      if (i0 >= rows) break;
-      load_rows(i0);
+    };
+    load_rows(0);                                         // (on their way while the angles are formed)
+    float wt[2][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) wt[0][e] = wt[1][e] = 1.f;
+    if (NORM == VC_NORM_HEAD && w) {
+      times_weights<T>(wt[0], a, w, at0);
+      times_weights<T>(wt[1], a, w, at1);
     }
-    float ss = lanes_sum((ch0 ? ss0 : 0.f) + (ch1 ? ss1 : 0.f), min(lanes << a.log_hl, 32));   // a token's lanes in this warp
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = ss;
-    __syncthreads();
-    const int warps = lanes << a.log_hl >> 5;                          // of a token; 0 or 1: its sum is at hand
-    if (warps > 1) {
-      ss = 0.f;
-      for (int i = 0; i < warps; ++i) ss += part[(threadIdx.x >> 5 & -warps) + i];   // one order for every thread of the token
+    if (ROT != VC_ROTARY_NONE && t == first) {
+      fill_table(a, tab, b, n0, tokens);
+      if (ROT == VC_ROTARY_HALF && threadIdx.x == 0) xch[kThreads * 16] = 0.f;
+      if constexpr (NORM != VC_NORM_TOKEN) __syncthreads();
     }
-    inv = rsqrtf(fmaf(ss, a.inv_count[t], a.eps));
-    if (rows > kKeep) load_rows(0);                                 // more heads than the registers hold: read twice
-  }
 
-  // cos and sin of my channels.  One that is not rotated keeps its value whatever its neighbour holds: bit e of `still`, or 0 in the
-  // place of the other half (with as many bits to test the predicate registers run out).
-  constexpr int kAngles = ROT >= VC_ROTARY_HALF ? 8 : 4;
-  float cs[2][kAngles], sn[2][kAngles];
-  int src[2][ROT == VC_ROTARY_HALF ? 8 : 1];
-  uint32_t still = 0;
-  const float2* mine = tab + tt * a.pairs;
-  const bool turned = ROT == kRotaryWhole && a.first_pair[c] != 255;
-  if constexpr (ROT == kRotaryWhole) {
-    const float4* from = reinterpret_cast<const float4*>(mine + (turned ? a.first_pair[c] : 0));      // (a multiple of eight pairs on)
+    float inv = 1.f;
+    if constexpr (NORM == VC_NORM_TOKEN) {
+      float ss0 = 0.f, ss1 = 0.f;
+      for (int i0 = 0;;) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float4 v = from[e];
-      cs[0][2 * e] = v.x; sn[0][2 * e] = v.y; cs[0][2 * e + 1] = v.z; sn[0][2 * e + 1] = v.w;
+        for (int i = 0; i < kKeep; ++i) {
+          if (i0 + i >= rows) break;
+          const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
+          if (i0 + i + 1 < rows || last_in) { ss0 += q0; ss1 += q1; }
+        }
+        i0 += kKeep;
+        if (i0 >= rows) break;
+        load_rows(i0);
+      }
+      float ss = lanes_sum((ch0 ? ss0 : 0.f) + (ch1 ? ss1 : 0.f), min(lanes << a.log_hl, 32));   // a token's lanes in this warp
+      if ((threadIdx.x & 31) == 0) part[t][threadIdx.x >> 5] = ss;
+      __syncthreads();
+      const int warps = lanes << a.log_hl >> 5;                          // of a token; 0 or 1: its sum is at hand
+      if (warps > 1) {
+        ss = 0.f;
+        for (int i = 0; i < warps; ++i) ss += part[t][(threadIdx.x >> 5 & -warps) + i];   // one order for every thread of the token
+      }
+      inv = rsqrtf(fmaf(ss, a.inv_count[t], a.eps));
+      if (rows > kKeep) load_rows(0);                                 // more heads than the registers hold: read twice
     }
-  } else if constexpr (ROT != VC_ROTARY_NONE) {
+
+    if (t == first) {
+      const float2* mine = tab + tt * a.pairs;
+      if constexpr (ROT == kRotaryWhole) {
+        const float4* from = reinterpret_cast<const float4*>(mine + (turned ? a.first_pair[c] : 0));      // (a multiple of eight pairs on)
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int cq = c + q * lanes;
+        for (int e = 0; e < 4; ++e) {
+          const float4 v = from[e];
+          cs[0][2 * e] = v.x; sn[0][2 * e] = v.y; cs[0][2 * e + 1] = v.z; sn[0][2 * e + 1] = v.w;
+        }
+      } else if constexpr (ROT != VC_ROTARY_NONE) {
 #pragma unroll
-      for (int e = 0; e < kAngles; ++e) {
-        cs[q][e] = 1.f; sn[q][e] = 0.f;
-        if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
-          const int p = 4 * cq + e;
-          if (p < a.pairs) { cs[q][e] = mine[p].x; sn[q][e] = mine[p].y; } else still |= 1u << (4 * q + e);
-        } else {
-          const int ch = 8 * cq + e;
-          src[q][e] = kThreads * 16 - r * 16 * lanes;
-          if (ch < 2 * a.pairs) {
-            const int axis = (ch >= 2 * a.pair_end[0]) + (ch >= 2 * a.pair_end[1]);
-            const int p0 = axis ? a.pair_end[axis - 1] : 0, half = a.pair_end[axis] - p0, i = ch - 2 * p0;
-            const bool low = i < half;
-            const int other = low ? ch + half : ch - half;
-            const float2 cosine_sine = mine[p0 + (low ? i : i - half)];
-            cs[q][e] = cosine_sine.x; sn[q][e] = low ? -cosine_sine.y : cosine_sine.y;
-            src[q][e] = (other & 7) * 2 * lanes + (other >> 3);
+        for (int q = 0; q < 2; ++q) {
+          const int cq = c + q * lanes;
+#pragma unroll
+          for (int e = 0; e < kAngles; ++e) {
+            cs[q][e] = 1.f; sn[q][e] = 0.f;
+            if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
+              const int p = 4 * cq + e;
+              if (p < a.pairs) { cs[q][e] = mine[p].x; sn[q][e] = mine[p].y; } else still |= 1u << (4 * q + e);
+            } else {
+              const int ch = 8 * cq + e;
+              src[q][e] = kThreads * 16 - r * 16 * lanes;
+              if (ch < 2 * a.pairs) {
+                const int axis = (ch >= 2 * a.pair_end[0]) + (ch >= 2 * a.pair_end[1]);
+                const int p0 = axis ? a.pair_end[axis - 1] : 0, half = a.pair_end[axis] - p0, i = ch - 2 * p0;
+                const bool low = i < half;
+                const int other = low ? ch + half : ch - half;
+                const float2 cosine_sine = mine[p0 + (low ? i : i - half)];
+                cs[q][e] = cosine_sine.x; sn[q][e] = low ? -cosine_sine.y : cosine_sine.y;
+                src[q][e] = (other & 7) * 2 * lanes + (other >> 3);
+              }
+            }
           }
         }
       }
     }
-  }
-  auto rotate = [&](float (&f)[2][8]) {
-    if constexpr (ROT == kRotaryWhole) {
-      if (turned) {
+    auto rotate = [&](float (&f)[2][8]) {
+      if constexpr (ROT == kRotaryWhole) {
+        if (turned) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float f0 = f[0][e], f1 = f[1][e];
+            f[0][e] = f0 * cs[0][e] - f1 * sn[0][e];
+            f[1][e] = f0 * sn[0][e] + f1 * cs[0][e];
+          }
+        }
+      } else if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          float g[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            g[2 * e] = f[q][2 * e] * cs[q][e] - f[q][2 * e + 1] * sn[q][e];
+            g[2 * e + 1] = f[q][2 * e] * sn[q][e] + f[q][2 * e + 1] * cs[q][e];
+          }
+          if (a.partial) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (still >> (4 * q + e / 2) & 1) g[e] = f[q][e];
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[q][e] = g[e];
+        }
+      } else if constexpr (ROT == VC_ROTARY_HALF) {
+        // a pair's halves are half an axis apart, in another lane as a rule: the head's channels change places in
+        // shared memory, element-major so that the lanes of an access lie side by side
+        float* row = xch + r * 16 * lanes;
+        __syncwarp();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float f0 = f[0][e], f1 = f[1][e];
-          f[0][e] = f0 * cs[0][e] - f1 * sn[0][e];
-          f[1][e] = f0 * sn[0][e] + f1 * cs[0][e];
+          row[e * 2 * lanes + c] = f[0][e];
+          row[e * 2 * lanes + c + lanes] = f[1][e];
         }
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[q][e] = f[q][e] * cs[q][e] + row[src[q][e]] * sn[q][e];
       }
-    } else if constexpr (ROT == VC_ROTARY_INTERLEAVED) {
+    };
+
+    int64_t w_at = (int64_t)hl * a.chunks * 8 + at0;
+    for (int i0 = 0; i0 < rows;) {
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        float g[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          g[2 * e] = f[q][2 * e] * cs[q][e] - f[q][2 * e + 1] * sn[q][e];
-          g[2 * e + 1] = f[q][2 * e] * sn[q][e] + f[q][2 * e + 1] * cs[q][e];
+      for (int i = 0; i < kKeep; ++i) {
+        if (i0 + i >= rows) break;
+        const bool in = i0 + i + 1 < rows || last_in;
+        float f[2][8];
+        raw[i][0].get(f[0]);
+        raw[i][1].get(f[1]);
+        if constexpr (NORM == VC_NORM_HEAD) {
+          const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
+          inv = rsqrtf(fmaf(lanes_sum((ch0 ? q0 : 0.f) + (ch1 ? q1 : 0.f), lanes), a.inv_count[t], a.eps));
         }
-        if (a.partial) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (still >> (4 * q + e / 2) & 1) g[e] = f[q][e];
+        if constexpr (NORM != VC_NORM_NONE) {
+          times(f[0], inv);
+          times(f[1], inv);
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[q][e] = g[e];
+        if constexpr (NORM == VC_NORM_HEAD) {
+          times(f[0], wt[0]);
+          times(f[1], wt[1]);
+        }
+        if constexpr (NORM == VC_NORM_TOKEN) {
+          if (w && in) {
+            times_weights<T>(f[0], a, w, w_at);
+            times_weights<T>(f[1], a, w, w_at + step);
+          }
+          w_at += (int64_t)a.chunks * 8 << a.log_hl;
+        }
+        rotate(f);
+        if (in) {
+          if (live0) store8<T>(y, f[0]);
+          if (live1) store8<T>(y + step, f[1]);
+        }
+        y += sy;
       }
-    } else if constexpr (ROT == VC_ROTARY_HALF) {
-      // a pair's halves are half an axis apart, in another lane as a rule: the head's channels change places in
-      // shared memory, element-major so that the lanes of an access lie side by side
-      float* row = xch + r * 16 * lanes;
-      __syncwarp();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        row[e * 2 * lanes + c] = f[0][e];
-        row[e * 2 * lanes + c + lanes] = f[1][e];
-      }
-      __syncwarp();
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[q][e] = f[q][e] * cs[q][e] + row[src[q][e]] * sn[q][e];
+      i0 += kKeep;
+      if (i0 < rows) load_rows(i0);
     }
   };
-
-  int64_t w_at = (int64_t)hl * a.chunks * 8 + at0;
-  for (int i0 = 0; i0 < rows;) {
-#pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      if (i0 + i >= rows) break;
-      const bool in = i0 + i + 1 < rows || last_in;
-      float f[2][8];
-      raw[i][0].get(f[0]);
-      raw[i][1].get(f[1]);
-      if constexpr (NORM == VC_NORM_HEAD) {
-        const float q0 = squares(raw[i][0]), q1 = squares(raw[i][1]);
-        inv = rsqrtf(fmaf(lanes_sum((ch0 ? q0 : 0.f) + (ch1 ? q1 : 0.f), lanes), a.inv_count[t], a.eps));
-      }
-      if constexpr (NORM != VC_NORM_NONE) {
-        times(f[0], inv);
-        times(f[1], inv);
-      }
-      if constexpr (NORM == VC_NORM_HEAD) {
-        times(f[0], wt[0]);
-        times(f[1], wt[1]);
-      }
-      if constexpr (NORM == VC_NORM_TOKEN) {
-        if (w && in) {
-          times_weights<T>(f[0], a, w, w_at);
-          times_weights<T>(f[1], a, w, w_at + step);
-        }
-        w_at += (int64_t)a.chunks * 8 << a.log_hl;
-      }
-      rotate(f);
-      if (in) {
-        if (live0) store8<T>(y, f[0]);
-        if (live1) store8<T>(y + step, f[1]);
-      }
-      y += sy;
-    }
-    i0 += kKeep;
-    if (i0 < rows) load_rows(i0);
+  if constexpr (NORM == VC_NORM_TOKEN) {
+#pragma unroll 1
+    for (int t = first; t <= last; ++t) side(t);
+  } else {
+    side(first);
   }
 }
 
@@ -314,7 +338,7 @@ constexpr double kTwoPi = 6.283185307179586476925286766559;
 // Frequencies of an axis's pairs in turns per position.  Powers by repeated multiplication, one call of pow() instead of one a pair
 // (1 us of a call's host time instead of 4): after i steps they are off by i / 2 units of 2^-52, but by then the frequency itself
 // has fallen so far that no angle is off by more than that of the first pairs.
-bool axis_frequencies(const vc_qk_params* p, int n, double factor, int original, double theta, double* out) {
+bool axis_frequencies(const vc_qk_params* p, int n, double factor, int original, double theta, uint64_t* out) {
   if (n == 0) return true;
   const int pairs = n / 2;
   if (p->rope_scaling == VC_ROPE_SCALING_NTK && n > 2) theta *= std::pow(factor, (double)n / (n - 2));
@@ -339,7 +363,7 @@ bool axis_frequencies(const vc_qk_params* p, int n, double factor, int original,
       r = r < 0 ? 0 : (r > 1 ? 1 : r);
       v = v * (1.0 - r) + v / factor * r;
     }
-    out[i] = v;
+    out[i] = (uint64_t)std::ldexp(v - std::floor(v), 64);       // (below 2^64: v below 1 has 53 bits)
   }
   return true;
 }
@@ -411,6 +435,7 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
         if ((int64_t)start[i] + grid[i] > INT32_MAX) return VC_ERR_INVALID_ARG;
       a.positions = nullptr;
       a.grid_h = p->grid_h; a.grid_w = p->grid_w;
+      a.inv_h = 1.0f / p->grid_h; a.inv_w = 1.0f / p->grid_w;
       for (int i = 0; i < 3; ++i) a.start[i] = start[i];
     }
     a.positions = positions;
@@ -455,7 +480,10 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
                                     (rows >> a.log_hl) >= 2 * p->N))
     ++a.log_hl;
   const int tokens = rows >> a.log_hl, tiles = (p->N + tokens - 1) / tokens;
-  const dim3 grid((unsigned)tiles, (unsigned)p->B, (unsigned)tensors);
+  // Long sequences under the norm over a token: one table of angles for Q and K (12 + 12 heads x 32760 x 128 99.9 -> 91.8 us; with the norm
+  // per head, where a CTA's phases are shorter, 85.2 -> 88.5).
+  a.both = p->norm == VC_NORM_TOKEN && tensors == 2 && (int64_t)p->B * tiles >= 16 * sm_count();
+  const dim3 grid((unsigned)tiles, (unsigned)p->B, a.both ? 1u : (unsigned)tensors);
   const size_t smem = rot == VC_ROTARY_NONE ? 0 : (size_t)tokens * a.pairs * sizeof(float2);
   cudaStream_t s = (cudaStream_t)stream;
   const cudaError_t e = p->dtype == VC_DTYPE_BF16   ? launch_norm<__nv_bfloat16>(p->norm, rot, a, grid, smem, s)

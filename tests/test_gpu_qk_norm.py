@@ -110,6 +110,24 @@ def test_factor_of_the_rotated_channels():
     _run(1, 2, 2, (9, 2, 2), 64, "fp32", "head", L.INTERLEAVED, (32, 0, 0), "yarn", (0.5, 1.0, 1.0), 64)      # no factor above 1: m = 1
 
 
+@pytest.mark.parametrize("layout,dims", [(L.INTERLEAVED, None), (L.HALF, None), (L.HALF, (64, 32, 32)), (None, None)])
+@pytest.mark.parametrize("Hq,Hk,grid", [(12, 3, (7, 23, 61)), (2, 11, (7, 23, 61)), (40, 40, (3, 40, 41))])
+def test_long_sequences_under_the_token_norm(layout, dims, Hq, Hk, grid):
+    """So many tokens that a CTA takes its tokens' queries and then their keys."""
+    _run(1, Hq, Hk, grid, 128, "bf16", "token", layout, dims)
+    _run(1, Hq, Hk, grid, 128, "fp16", "token", layout, dims, in_place=True)
+
+
+@pytest.mark.parametrize("layout", [L.INTERLEAVED, L.HALF])
+def test_positions_over_the_whole_range_of_int32(layout):
+    """The angle in FP64 is off by 2^31 2^-53 there: nothing beside a step of bf16."""
+    rng = np.random.default_rng(12)
+    pos = rng.integers(-2 ** 31, 2 ** 31, size=(2, 300, 3))
+    pos[:, :4] = [[[-2 ** 31] * 3, [2 ** 31 - 1] * 3, [-1] * 3, [0] * 3]]
+    _run(2, 2, 1, (300, 1, 1), 64, "bf16", "none", layout, (16, 32, 16), positions=pos)
+    _run(1, 2, 1, (300, 1, 1), 64, "bf16", "head", layout, (16, 32, 16), start=(2 ** 31 - 400, 5, 2 ** 30))
+
+
 @pytest.mark.parametrize("layout", [L.INTERLEAVED, L.HALF])
 def test_positions_from_an_array(layout):
     rng = np.random.default_rng(3)
