@@ -92,6 +92,54 @@ def test_tiles_of_two_ctas(M, N, splits):
     _check(M, N, 16, "fp16", bias=False, k_splits=splits)
 
 
+@pytest.mark.parametrize("M,N", [(1300, 1800), (1409, 1665), (1500, 1630), (5000, 2000), (4609, 1665)])
+@pytest.mark.parametrize("splits", [0, 3])
+def test_fewer_rounds_by_pairs_of_ctas(M, N, splits):
+    """Sizes at which a tile is two CTAs': the last one with a CTA without rows or with one, weights that end in either half, up to three tiles a pair."""
+    _check(M, N, 400, "bf16", k_splits=splits)
+    _check(M, N, 16, "fp16", bias=False, k_splits=splits)
+    _check(M, N, 272, "fp32", bias_dt="bf16", k_splits=splits)
+
+
+@pytest.mark.parametrize("N", [1800, 1801])
+def test_pairs_of_ctas_leave_neighbours_alone(N):
+    M, K = 1301, 144
+    x, xs, w, ws = _operands(M, N, K, 6)
+    wide_x, wide_w = np.full((M + 3, K + 32), 0x7f, np.uint8), np.full((N + 5, K + 48), 0x7f, np.uint8)      # NaN codes around
+    wide_x[:M, :K], wide_w[:N, :K] = x, w
+    around = torch.full((M + 4, N + 24), -7.0, dtype=DT["bf16"], device="cuda")
+    out = _run(_dev(wide_x)[:M, :K], _dev(xs), _dev(wide_w)[:N, :K], _dev(ws), "bf16", out=around[:M, 8:N + 8])
+    _close(out, x, xs, w, ws, "bf16")
+    assert (around[M:] == -7).all() and (around[:, :8] == -7).all() and (around[:, N + 8:] == -7).all()
+
+
+@pytest.mark.parametrize("K", [1024, 16384])
+def test_wait_of_a_pair_of_ctas_that_runs_out(K):
+    """As below, for both CTAs: they end together, and the next call is right."""
+    g = torch.Generator().manual_seed(14)
+    M, N = 2300, 1800
+    x, w = (torch.randint(0, 120, (n, K), generator=g, dtype=torch.uint8).cuda() for n in (M, N))
+    xs, ws = torch.rand(K // 128, M, generator=g).cuda(), torch.rand(-(-N // 128), K // 128, generator=g).cuda()
+    want = _run(x, xs, w, ws, "bf16")
+    out = torch.empty_like(want)
+    p = vc.LinearParams.of(x, w, out)
+    work = torch.empty(vc.vc_linear_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    code = vc.VC_OK
+    try:
+        vc.vc_test_set_wait_limit(1)
+        vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)
+        vc.vc_poll_status(work)
+    except vc.VcError as e:
+        code = e.code
+    finally:
+        vc.vc_test_set_wait_limit(0)
+    assert code == vc.VC_ERR_TIMEOUT or (K == 1024 and code == vc.VC_OK and torch.equal(out, want))
+    for _ in range(3):
+        vc.vc_linear_fp8(p, x, xs, w, ws, None, out, work)
+        vc.vc_poll_status(work)
+        assert torch.equal(out, want)
+
+
 @pytest.mark.parametrize("M", [5, 50, 200, 2500])
 def test_rows_of_wider_matrices_and_neighbours(M):
     N, K = 2500, 160
