@@ -8,7 +8,8 @@
 //
 // Three shapes: tiles of 256 x 256 by two CTAs of a cluster (each 128 rows of A and half of B in shared memory, 128 rows of sums), where
 // these fill the SMs; tiles of 128 x 128; and up to 64 rows of x as B with 128 weight rows as A, which is bound by reading the weights.  With
-// fewer tiles than SMs the blocks of K are split between CTAs and the parts joined by a second launch in a fixed order.
+// fewer tiles than SMs the blocks of K are split between CTAs and the parts joined in a fixed order: up to 64 rows by a cluster of the CTAs, from shared
+// memory, else by a second launch.
 //
 // What bounds the large ones: per block the tensor cores need 512 cycles, 128 x 256 sums out of tensor memory 256 and their additions
 // 256 of the FMA pipe, side by side; but there are two buffers only (256 columns each of 512), and a buffer's round, product 512, signal 100,
@@ -19,7 +20,7 @@
 // 128 columns (two products of 256 x 128 a block, A read twice): 794, and 868 under the cap.  A release or acquire of
 // cluster scope at the buffers' barriers: 1490 (it waits for every load in flight).  Packed additions: 860 (a move and a half each, the products
 // arrive in registers that do not pair up).  Four warpgroups of 64 columns, scales four blocks ahead: no gain.
-// 5120 x 5120 with weights in L2: one row 8.1 us (two launches; 26 MB at the copy rate 4.0), 512 rows 22, 1024 rows 40.
+// 5120 x 5120 with weights in L2: one row 7.7 us (26 MB at the copy rate 4.0), 512 rows 22, 1024 rows 40.
 #include "vc_attn_shared.cuh"
 #include "vc_layer.cuh"
 #include "vc_sm100.cuh"
@@ -31,6 +32,7 @@ using namespace layer;
 using namespace sm100;
 
 constexpr int kThreads = 384;
+constexpr int kCluster = 8;                  // CTAs of a portable cluster
 constexpr int kSms = 148;                    // what the rule for splits counts on: the workspace's size must not vary
 
 struct LinearArgs {
@@ -43,6 +45,7 @@ struct LinearArgs {
   int M, N, blocks, tiles_b, splits, items;  // blocks: of 128 columns of K; tiles_b: tiles along B
   int out_dtype, bias_dtype;
   bool vec;                                  // rows of out start on 16-byte boundaries
+  bool joined;                               // the CTAs of a tile's splits are a cluster and join their sums themselves
   uint32_t limit, nonblocking;
 };
 
@@ -111,6 +114,13 @@ __device__ __forceinline__ uint32_t in_leader(const void* p) {       // the addr
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ float4 load_cluster(const float4* p, int rank) {    // from the same place of the cluster's CTA `rank`
+  uint32_t at;
+  float4 v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
@@ -228,7 +238,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     }
   }
   if (tid == 0 && blockIdx.x == 0) *a.status = 0;
-  if (a.splits > 1) pdl_allow();               // (what follows then is the launch that joins the parts: it may stand by)
+  if (a.splits > 1 && !a.joined) pdl_allow();               // (what follows then is the launch that joins the parts: it may stand by)
   tc_fence_before();
   if constexpr (C::kPair) cluster_sync(); else __syncthreads();
   tc_fence_after();
@@ -403,7 +413,10 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
       }
       if constexpr (SWAP) {
         const int col = now.a0 + row;
-        if (col < a.N) {
+        if (a.joined) {                            // (the last product is complete: the stages are free)
+#pragma unroll
+          for (int i = 0; i < kCols; ++i) reinterpret_cast<float*>(smem)[i * 128 + row] = y[i];
+        } else if (col < a.N) {
 #pragma unroll
           for (int i = 0; i < kCols; ++i) {
             if (m0 + i >= a.M) break;
@@ -436,6 +449,36 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");       // the rows have left shared memory before the CTA may end
   }
   tc_fence_before();
+  if (SWAP && a.joined) {
+    // A sum's parts in the order of the splits, from the shared memory of the cluster's CTAs, each of which takes some of the sums.
+    const Item w = item_of<TN>(a, first, rank);
+    const int rows = min(TN, a.M - w.b0);
+    cluster_sync();
+    for (int e = w.split * kThreads + tid; e < rows * 32; e += a.splits * kThreads) {        // four columns of a row
+      const int col = w.a0 + 4 * (e & 31);
+      if (col >= a.N) continue;
+      float4 v[kCluster];
+      float y[4] = {};
+#pragma unroll
+      for (int i = 0; i < kCluster; ++i)
+        if (i < a.splits) v[i] = load_cluster(reinterpret_cast<const float4*>(smem) + e, i);
+#pragma unroll
+      for (int i = 0; i < kCluster; ++i)
+        if (i < a.splits) { y[0] += v[i].x; y[1] += v[i].y; y[2] += v[i].z; y[3] += v[i].w; }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (col + j >= a.N) break;
+        if (a.bias) y[j] += load1(a.bias, a.bias_dtype, col + j);
+        const int64_t at = (w.b0 + (e >> 5)) * a.ldo + col + j;
+        if (a.out_dtype == VC_DTYPE_BF16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(y[j]);
+        else if (a.out_dtype == VC_DTYPE_FP16) static_cast<__half*>(a.out)[at] = __float2half_rn(y[j]);
+        else static_cast<float*>(a.out)[at] = y[j];
+      }
+    }
+    cluster_sync();                            // (a CTA stays until its peers have read it)
+    if (warp == 10) tmem_dealloc<C::kTmem>(tmem);
+    return;
+  }
   if constexpr (C::kPair) {
     cluster_sync();                            // (neither CTA ends, nor gives its tensor memory back, while the other's products or signals reach it)
     if (warp == 10) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(C::kTmem) : "memory");
@@ -471,11 +514,14 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
 }
 
 struct Plan {
-  bool swap;
+  bool swap, joined;
   int tn, tiles_b, splits, blocks;
   int64_t items, ldp;
   size_t total;
 };
+
+// Clusters of n CTAs with an SM each that run side by side: eight GPCs of 18 SMs or more.
+inline int clusters_at_once(int n) { return 8 * (18 / n); }
 
 vc_status resolve(const vc_linear_params* p, vc_linear_params* out, Plan* plan) {
   if (!p) return VC_ERR_INVALID_ARG;
@@ -504,9 +550,16 @@ vc_status resolve(const vc_linear_params* p, vc_linear_params* out, Plan* plan) 
     const int64_t room = kSms / (tiles * ctas);
     pl.splits = 1;
     if (room > 1 && pl.blocks >= 8) pl.splits = (int)(room < pl.blocks / 4 ? room : pl.blocks / 4);
+    if (pl.swap) {                             // no more than clusters of as many CTAs find room for at a time
+      if (pl.splits > kCluster) pl.splits = kCluster;
+      while (pl.splits > 1 && tiles > clusters_at_once(pl.splits)) --pl.splits;
+    }
   }
   if (pl.splits > pl.blocks) pl.splits = pl.blocks;
   if (pl.splits > 64) pl.splits = 64;
+  // Few rows: the splits of a tile are a cluster and need no second launch (one row of 5120 x 5120 8.2 -> 7.7 us, 64 rows 11.8 -> 10.8,
+  // one row of 1536 x 8960 7.8 -> 6.7).
+  pl.joined = pl.swap && pl.splits > 1 && pl.splits <= kCluster && tiles <= clusters_at_once(pl.splits);
   pl.items = tiles * pl.splits;
   if (pl.items > INT32_MAX) return VC_ERR_UNSUPPORTED;
   pl.ldp = (r.N + 3) / 4 * 4ll;
@@ -549,13 +602,13 @@ cudaError_t launch_linear(const vc_linear_params& r, const Plan& pl, const Linea
   if (!SWAP && a.vec && pl.splits == 1 && !make_map_out(&to, a.out, r)) return cudaErrorUnknown;
   cudaError_t e = allow_smem<linear_fp8_kernel<SWAP, TN>>();
   if (e != cudaSuccess) return e;
-  constexpr int kCtas = C::kPair ? 2 : 1;
-  const int room = sm_count() / kCtas, grid = kCtas * (pl.items < room ? (int)pl.items : room);
+  const int ctas = C::kPair ? 2 : pl.joined ? pl.splits : 1, room = sm_count() / (C::kPair ? 2 : 1);
+  const int grid = pl.joined ? (int)pl.items : (C::kPair ? 2 : 1) * (pl.items < room ? (int)pl.items : room);       // (joined: an item a CTA)
   constexpr size_t smem = C::kStages * C::kStage + C::kOut + sizeof(Smem<C::kStages, C::kBufs>);
-  e = launch_clusters(linear_fp8_kernel<SWAP, TN>, dim3((unsigned)grid), kCtas, kThreads, smem, s, ta, tb, to, a);
+  e = launch_clusters(linear_fp8_kernel<SWAP, TN>, dim3((unsigned)grid), ctas, kThreads, smem, s, ta, tb, to, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
-  if (pl.splits > 1) {
+  if (pl.splits > 1 && !pl.joined) {
     const int64_t work = ((int64_t)r.M * ((r.N + 3) / 4) + 255) / 256, most = 8 * sm_count();
     e = launch_overlapped(linear_join_kernel, dim3((unsigned)(work < most ? work : most)), 256, 0, s, a);
     if (e != cudaSuccess) return e;
@@ -590,7 +643,7 @@ extern "C" vc_status vc_linear_fp8(const vc_linear_params* p, const void* x_code
   a.status = (uint32_t*)workspace;
   a.part = (float*)((uint8_t*)workspace + 256);
   a.ldo = r.ldo; a.ldp = pl.ldp;
-  a.M = r.M; a.N = r.N; a.blocks = pl.blocks; a.tiles_b = pl.tiles_b; a.splits = pl.splits; a.items = (int)pl.items;
+  a.M = r.M; a.N = r.N; a.blocks = pl.blocks; a.tiles_b = pl.tiles_b; a.splits = pl.splits; a.joined = pl.joined; a.items = (int)pl.items;
   a.out_dtype = r.out_dtype; a.bias_dtype = r.bias_dtype;
   a.vec = r.ldo * elem_size(r.out_dtype) % 16 == 0;
   a.limit = attn::attn_wait_limit();

@@ -101,6 +101,13 @@ def test_fewer_rounds_by_pairs_of_ctas(M, N, splits):
     _check(M, N, 272, "fp32", bias_dt="bf16", k_splits=splits)
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 5120, 5120), (16, 1, 4096), (17, 640, 2064), (64, 1537, 1024), (33, 130, 5120)])
+@pytest.mark.parametrize("splits", [0, 2, 3, 7, 8, 9])
+def test_parts_joined_by_a_cluster_and_by_a_launch(M, N, K, splits):
+    _check(M, N, K, "bf16", k_splits=splits)
+    _check(M, N, K, "fp32", bias=False, k_splits=splits)
+
+
 @pytest.mark.parametrize("N", [1800, 1801])
 def test_pairs_of_ctas_leave_neighbours_alone(N):
     M, K = 1301, 144
