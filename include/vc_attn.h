@@ -403,8 +403,8 @@ vc_status vc_qk_norm_rope(const vc_qk_params *p, const void *q, const void *k, c
  * the row is 0 and its lse -infinity.  H_kv divides H: heads h of Q with the same h / (H / H_kv) share keys and values.
  * Scores, maxima, sums and the output's accumulators are FP32; probabilities are rounded to the tensors' type in front of
  * the second product, as its operand.  lse: fp32 [B][H][N_q], or NULL.
- * Few rows against many keys: the keys of a row are split between CTAs and joined by a second launch, in a
- * fixed order; key_splits = 1 forbids it, 0 leaves the number to the library.
+ * Few rows against many keys: the keys of a row are split between CTAs and joined in a fixed order, by a
+ * second launch where the parts are many; key_splits = 1 forbids it, 0 leaves the number to the library.
  * workspace: vc_cross_workspace_bytes(p) bytes; contents on entry irrelevant, its first 4 bytes become the status word
  * (vc_poll_status).  Calls that may overlap need workspaces of their own. */
 typedef struct {

@@ -49,6 +49,7 @@ struct CrossArgs {
   int qtiles, qitems, tiles_per_item, splits, items;
   int q_b, q_h, k_b, k_h, v_b, v_h;               // 1, or 0 for a dimension that is broadcast: multiplies the copy's coordinate
   float sl;                                       // softmax_scale * log2(e)
+  bool joined;                                    // the CTAs of a tile's splits are a cluster and join their parts themselves
   uint32_t limit, nonblocking;
 };
 
@@ -113,6 +114,19 @@ template <typename T> __device__ constexpr uint32_t idesc16(int M, int N) {     
   return (1u << 4) | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// N floats from the same place of the shared memory of the cluster's CTA `rank`.
+template <int N> __device__ __forceinline__ void load_cluster(const float* p, int rank, float (&v)[N]) {
+  uint32_t at;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  if constexpr (N == 4) asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at) : "memory");
+  else if constexpr (N == 2) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(at) : "memory");
+  else asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[0]) : "r"(at) : "memory");
+}
+
+constexpr int kCluster = 8;                       // CTAs of a portable cluster
 constexpr uint32_t kPanel = 128 * 128;            // 128 rows of 64 16-bit channels
 
 template <int D> struct Lay {
@@ -132,6 +146,8 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                   const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ CrossArgs a) {
   using L = Lay<D>;
   constexpr int kRegSoftmax = 176, kRegEpi = 80, kRegCtl = 80;
+  constexpr int kPartRow = D + 4;              // floats from row to row of a part in shared memory: no bank conflicts
+  static_assert((128 * kPartRow + 128) * 4 <= kStages * L::kTile, "a part exceeds the ring");
   static_assert(2 * kRegSoftmax + kRegEpi + kRegCtl <= 4 * 128, "register budget exceeds the CTA's allocation");
   static_assert(L::kSmem <= 227 * 1024, "shared memory of the kernel exceeds the SM");
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -158,7 +174,7 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   pdl_wait();
   if (warp == 2) { tmem_alloc<512>(&sh->tmem_base); tmem_relinquish(); }
   if (tid == 0 && blockIdx.x == 0) *a.status = 0;
-  if (a.splits > 1) pdl_allow();               // (what follows then is the launch that joins the parts: it may stand by)
+  if (a.splits > 1 && !a.joined) pdl_allow();               // (what follows then is the launch that joins the parts: it may stand by)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -526,7 +542,8 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             for (int i = 0; i < 32; ++i) r[i] = 0;
           }
           if (a.splits > 1) {
-            float4* po = reinterpret_cast<float4*>(a.part_o + line * D + 32 * c);
+            // (joined: the last product is complete, the ring is free)
+            float4* po = reinterpret_cast<float4*>(a.joined ? reinterpret_cast<float*>(sKV) + (quarter * 32 + lane) * kPartRow + 32 * c : a.part_o + line * D + 32 * c);
             if (lane < rows)
 #pragma unroll
               for (int i = 0; i < 32; i += 4)
@@ -552,7 +569,8 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           }
         }
         if (lane < rows) {
-          if (a.splits > 1) a.part_lse[line] = lse2;
+          if (a.joined) reinterpret_cast<float*>(sKV)[128 * kPartRow + quarter * 32 + lane] = lse2;
+          else if (a.splits > 1) a.part_lse[line] = lse2;
           else if (a.lse) a.lse[line] = lse2 * kLn2;
         }
       }
@@ -560,6 +578,43 @@ cross_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");       // the rows have left shared memory before the CTA may end
   }
   tc_fence_before();
+  if (HALVES && a.joined) {
+    // A row's parts in the order of the splits (as cross_join_kernel), from the shared memory of the cluster's CTAs.  A warp a row.
+    constexpr int kPer = D / 32;
+    const Item w = item_of(a, blockIdx.x);
+    const int rows = min(128, a.Nq - w.q0 * 128);
+    const float* part = reinterpret_cast<const float*>(sKV);
+    cluster_sync();
+    for (int r = w.split * (kThreads / 32) + warp; r < rows; r += a.splits * (kThreads / 32)) {
+      float lse[kCluster][1], po[kCluster][kPer], top = -INFINITY, acc[kPer] = {}, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kCluster; ++i)
+        if (i < a.splits) {
+          load_cluster<1>(part + 128 * kPartRow + r, i, lse[i]);
+          load_cluster<kPer>(part + r * kPartRow + lane * kPer, i, po[i]);
+        }
+#pragma unroll
+      for (int i = 0; i < kCluster; ++i)
+        if (i < a.splits) top = lse[i][0] != lse[i][0] || top != top ? NAN : fmaxf(top, lse[i][0]);
+      const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < kCluster; ++i)
+        if (i < a.splits) {
+          const float wt = exp2f(lse[i][0] - base);
+          sum += wt;
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) acc[j] = fmaf(wt, po[i][j], acc[j]);
+        }
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      T* dst = static_cast<T*>(a.o) + w.b * a.so.b + w.h * a.so.h + (int64_t)(w.q0 * 128 + r) * a.so.n + lane * kPer;
+#pragma unroll
+      for (int j = 0; j < kPer; j += 2) reinterpret_cast<uint32_t*>(dst)[j / 2] = pack16<T>(acc[j] * inv, acc[j + 1] * inv);
+      if (a.lse && lane == 0) a.lse[((int64_t)w.b * a.H + w.h) * a.Nq + w.q0 * 128 + r] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * kLn2;
+    }
+    cluster_sync();                            // (a CTA stays until its peers have read it)
+    if (warp == 2) tmem_dealloc<512>(tmem);
+    return;
+  }
   __syncthreads();
   if (warp == 2) tmem_dealloc<512>(tmem);
 }
@@ -596,7 +651,11 @@ cross_join_kernel(const __grid_constant__ CrossArgs a, int64_t rows) {
   if (a.lse && lane == 0) a.lse[r] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * kLn2;
 }
 
+// Clusters of n CTAs with an SM each that run side by side: eight GPCs of 18 SMs or more.
+inline int clusters_at_once(int n) { return 8 * (18 / n); }
+
 struct Plan {
+  bool joined;
   int qtiles, tiles_per_item, qitems, splits;
   int64_t rows, items;
   size_t part_o, part_lse, total;
@@ -634,6 +693,10 @@ vc_status resolve(const vc_cross_params* p, vc_cross_params* out, Plan* plan) {
   }
   if (pl.splits > ktiles) pl.splits = ktiles > 0 ? ktiles : 1;
   if (pl.splits > 64) pl.splits = 64;
+  // Few parts: the splits of a tile are a cluster and need no second launch (B2 H16, one token against 16384 keys 50.5 -> 49.1 us, B4 H8 against 2048
+  // 12.7 -> 11.4, B1 H12, 100 against 2048 14.3 -> 13.6), up to two rows a warp of the cluster (four, 128 rows in two parts: 11.8 -> 12.9).
+  pl.joined = pl.tiles_per_item == 1 && pl.splits > 1 && pl.splits <= kCluster && bh * pl.qitems <= clusters_at_once(pl.splits) &&
+              (r.N_q < 128 ? r.N_q : 128) <= 32 * pl.splits;
   pl.items = bh * pl.qitems * pl.splits;
   if (pl.items > INT32_MAX) return VC_ERR_UNSUPPORTED;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -669,11 +732,11 @@ cudaError_t launch_cross(const vc_cross_params& r, const Plan& pl, CrossArgs& a,
     return cudaErrorUnknown;
   cudaError_t e = allow_smem<cross_attn_kernel<T, D, HALVES>>();
   if (e != cudaSuccess) return e;
-  const int grid = pl.items < sm_count() ? (int)pl.items : sm_count();
-  e = launch_overlapped(cross_attn_kernel<T, D, HALVES>, dim3((unsigned)grid), kThreads, Lay<D>::kSmem, s, tq, tk, tv, to, a);
+  const int grid = pl.joined || pl.items < sm_count() ? (int)pl.items : sm_count();       // (joined: an item a CTA)
+  e = launch_clusters(cross_attn_kernel<T, D, HALVES>, dim3((unsigned)grid), pl.joined ? pl.splits : 1, kThreads, Lay<D>::kSmem, s, tq, tk, tv, to, a);
   if (e != cudaSuccess) return e;
   count_launches(1);
-  if (pl.splits > 1) {
+  if (pl.splits > 1 && !pl.joined) {
     e = launch_overlapped(cross_join_kernel<T, D>, dim3((unsigned)((pl.rows + 7) / 8)), 256, 0, s, a, pl.rows);
     if (e != cudaSuccess) return e;
     count_launches(1);
@@ -714,7 +777,7 @@ extern "C" vc_status vc_cross_attn(const vc_cross_params* p, const void* q, cons
   a.part_lse = (float*)((uint8_t*)workspace + pl.part_lse);
   a.so = r.o;
   a.heads = r.B * r.H; a.H = r.H; a.group = r.H / r.H_kv; a.Nq = r.N_q; a.Nkv = r.N_kv;
-  a.qtiles = pl.qtiles; a.qitems = pl.qitems; a.tiles_per_item = pl.tiles_per_item; a.splits = pl.splits; a.items = (int)pl.items;
+  a.qtiles = pl.qtiles; a.qitems = pl.qitems; a.tiles_per_item = pl.tiles_per_item; a.splits = pl.splits; a.joined = pl.joined; a.items = (int)pl.items;
   a.sl = r.softmax_scale * kLog2e;
   a.limit = attn::attn_wait_limit();
   a.nonblocking = attn::attn_wait_nonblocking();

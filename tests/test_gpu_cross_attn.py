@@ -116,6 +116,32 @@ def test_heads_of_one_query_tile(dt, d, H, Nq):
     _check(q, k, v, o, lse, lens, mask.cuda())
 
 
+@pytest.mark.parametrize("dt,d", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("splits", [2, 3, 7, 8, 9])
+@pytest.mark.parametrize("Nq", [1, 64, 100, 129])
+def test_parts_joined_by_a_cluster_and_by_a_launch(dt, d, splits, Nq):
+    """Parts without a key, rows whose keys are all masked."""
+    B, H, N = 2, 4, 1300
+    g = torch.Generator().manual_seed(splits + Nq + d)
+    q, k, v = _heads(B, H, Nq, d, dt, g, True, 2.0), _heads(B, 2, N, d, dt, g, True), _heads(B, 2, N, d, dt, g, True)
+    lens = torch.tensor([1300, 400], dtype=torch.int32, device="cuda")
+    mask = torch.rand(B, N, generator=g) < 0.6
+    mask[1, :256] = False
+    for a in ((), (lens,), (lens, mask.cuda()), (None, torch.zeros_like(mask).cuda())):
+        o, lse = _call(q, k, v, *a, key_splits=splits)
+        _check(q, k, v, o, lse, *a)
+
+
+def test_nan_of_one_part_reaches_the_row():
+    g = torch.Generator().manual_seed(31)
+    q, k, v = _heads(1, 2, 3, 128, "bf16", g), _heads(1, 2, 1000, 128, "bf16", g), _heads(1, 2, 1000, 128, "bf16", g)
+    q[0, 1, 2, 5] = float("nan")
+    for splits in (1, 4):
+        o, lse = _call(q, k, v, key_splits=splits)
+        bad = torch.isnan(o).all(-1)
+        assert bad[0, 1, 2] and bad.sum() == 1 and torch.isfinite(o[~bad]).all() and torch.isnan(lse).sum() == 1
+
+
 @pytest.mark.parametrize("splits", [5, 6, 12])
 @pytest.mark.parametrize("Nq", [1, 200])
 def test_many_parts_of_keys(splits, Nq):
