@@ -344,7 +344,8 @@ enum { VC_DTYPE_BF16 = 0, VC_DTYPE_FP16 = 1, VC_DTYPE_FP32 = 2 };
 
 /* Strides of a [B][H][N][d] tensor in elements, d contiguous; all 0 = packed.  Every row must start on a 16-byte
  * boundary: the base pointer does, and each stride is a multiple of 16 bytes (a stride of 0 beside others that
- * are not is a broadcast, for inputs only). */
+ * are not is a broadcast, for inputs only).  The rows of an output do not overlap: its dimensions of more than one entry, taken by
+ * stride, each step over all that the smaller ones span. */
 typedef struct { int64_t b, h, n; } vc_strides;
 
 /* Norm of queries and keys and their position rotation, in one pass over both.

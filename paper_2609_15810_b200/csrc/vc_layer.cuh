@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <utility>
+
 #include "vc_internal.h"
 #include "vc_launch.h"
 #include "vc_sm100.cuh"
@@ -18,8 +20,9 @@ inline bool bad_dtype(int dtype) { return dtype < VC_DTYPE_BF16 || dtype > VC_DT
 inline bool misaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 // Strides of [B][H][N][d] with the packed default filled in; those of dimensions of one entry are never used and are
-// made harmless.  Refuses rows off a 16-byte boundary, rows that overlap, and (for outputs) broadcasts.  Strides stay below 2^40 bytes
-// and the tensor below 2^60, so that no address computed from them wraps.
+// made harmless.  Refuses rows off a 16-byte boundary and tokens that overlap, for outputs any two rows that might: taken by
+// stride, each dimension must step over what the smaller ones span (a broadcast, stride 0, does not).  Strides stay below 2^40
+// bytes, so that the span of an output (2^22 tokens, 65535 heads and batches at most) stays below 2^63.
 inline bool resolve_strides(const vc_strides& in, int64_t B, int64_t H, int64_t N, int64_t d, int es, bool output, vc_strides* out) {
   vc_strides s = in;
   if (!s.b && !s.h && !s.n) { s.n = d; s.h = N * d; s.b = H * N * d; }
@@ -30,7 +33,18 @@ inline bool resolve_strides(const vc_strides& in, int64_t B, int64_t H, int64_t 
   if (s.b < 0 || s.h < 0 || s.n < d) return false;
   if (s.b >= most || s.h >= most || s.n >= most) return false;
   if (s.b % per16 || s.h % per16 || s.n % per16) return false;
-  if (output && ((B > 1 && s.b == 0) || (H > 1 && s.h == 0))) return false;
+  if (output) {
+    struct { int64_t count, stride; } dim[3] = {{B, s.b}, {H, s.h}, {N, s.n}};
+    for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < 2 - i; ++j)
+        if (dim[j].stride > dim[j + 1].stride) std::swap(dim[j], dim[j + 1]);
+    int64_t span = d;
+    for (const auto& m : dim) {
+      if (m.count == 1) continue;
+      if (m.stride < span) return false;
+      span += (m.count - 1) * m.stride;
+    }
+  }
   *out = s;
   return true;
 }

@@ -48,6 +48,15 @@ def test_qk_norm_rope_in_place_wants_the_same_strides():
     assert _qk(ptrs=(P, P, P, P, None, P, 2 * P), q_out=Strides(0, 64, 128)) == vc.VC_ERR_INVALID_ARG
 
 
+OVERLAPPING = [Strides(0, 8, 64), Strides(0, 64, 64), Strides(0, 64, 72), Strides(0, 64 * 23, 64), Strides(0, 128, 64)]
+
+
+@pytest.mark.parametrize("at", range(len(OVERLAPPING)))
+@pytest.mark.parametrize("name", ["q_out", "k_out"])
+def test_qk_norm_rope_outputs_whose_heads_overlap(name, at):
+    assert _qk(ptrs=NO_POS, **{name: OVERLAPPING[at]}) == vc.VC_ERR_INVALID_ARG
+
+
 def _quant(x=P, codes=P, scale=P, **kw):
     p = QuantParams(B=1, H=2, N=5, d=64, block_rows=1)
     for k, v in kw.items():
@@ -99,6 +108,39 @@ def test_cross_attn_workspace():
     assert size(key_splits=64) == size(key_splits=32)            # no more than there are key tiles
     assert size(N_kv=0) == size(N_kv=128) == 256
     assert size() >= 256 and size(N_q=100000) == 256             # enough rows: nothing to split
+
+
+@pytest.mark.parametrize("o", [
+    Strides(20 * 64, 8, 64), Strides(20 * 64, 64, 64), Strides(20 * 64, 64, 128), Strides(20 * 64, 4 * 64, 64), Strides(19 * 64, 5 * 64, 64),
+    Strides(64, 5 * 64, 64), Strides(8, 5 * 64, 64), Strides(20 * 64, 64, 4 * 64 - 8)])
+def test_cross_attn_outputs_whose_heads_or_batches_overlap(o):
+    p = CrossParams(B=2, H=4, H_kv=2, N_q=5, N_kv=7, d=64, o=o)
+    assert vc.load_library().vc_cross_attn(ctypes.byref(p), P, P, P, P, P, P, P, P, None) == vc.VC_ERR_INVALID_ARG
+    assert vc.vc_cross_workspace_bytes(p) == 0
+
+
+@pytest.mark.parametrize("o", [
+    Strides(20 * 64, 5 * 64, 64), Strides(20 * 64, 64, 4 * 64), Strides(64, 2 * 64, 8 * 64), Strides(64, 10 * 64, 2 * 64), Strides(4 * 64, 64, 8 * 64),
+    Strides(2 ** 39 - 8, 72, 4 * 72)])
+def test_cross_attn_outputs_in_any_order_of_dimensions(o):
+    assert vc.vc_cross_workspace_bytes(CrossParams(B=2, H=4, H_kv=2, N_q=5, N_kv=7, d=64, o=o)) == 256
+
+
+def test_cross_attn_inputs_whose_heads_overlap_are_read():
+    p = CrossParams(B=2, H=4, H_kv=2, N_q=5, N_kv=7, d=64, q=Strides(0, 8, 64), k=Strides(64, 64, 64), v=Strides(0, 0, 64))
+    assert vc.vc_cross_workspace_bytes(p) == 256
+
+
+@pytest.mark.parametrize("kw", [dict(B=1), dict(H=1, H_kv=1), dict(N_q=1)])
+def test_cross_attn_strides_of_dimensions_of_one_entry_are_not_looked_at(kw):
+    """With one batch, head or query its stride overlaps nothing."""
+    at = {"B": "b", "H": "h", "N_q": "n"}[next(iter(kw))]
+    o = Strides(20 * 64, 5 * 64, 64)
+    setattr(o, at, 8)
+    p = CrossParams(B=2, H=4, H_kv=2, N_q=5, N_kv=7, d=64, o=o)
+    for n, val in kw.items():
+        setattr(p, n, val)
+    assert vc.vc_cross_workspace_bytes(p) == 256
 
 
 def _linear(ptrs=(P,) * 7, **kw):
