@@ -52,8 +52,9 @@ __device__ __forceinline__ int quotient(int n, int by, float inv) {
 }
 
 // Angles of the CTA's tokens.  The product of position and frequency is formed in 64-bit fixed point, whose overflow takes off the whole
-// turns: its error is 2^-33 turns at most (in FP32 the angle of position 10^5 is off by 10^-2; in FP64, with the integer
-// divisions of the position, a table took twice as long: 12 + 12 heads x 32760 x 128, norm per head, 94.3 us instead of 85.2).
+// turns: at position p it is off by |p| 2^-64 turns, and by p times what the frequency is off by (see axis_frequencies; together below 2^-27 at
+// position 2^31).  Rounding it to FP32 for the sine, up to 2^-26 turns, is more.  (In FP32 the angle of position 10^5 is off by 10^-2; in FP64, with the
+// integer divisions of the position, a table took twice as long: 12 + 12 heads x 32760 x 128, norm per head, 94.3 us instead of 85.2.)
 __device__ __forceinline__ void fill_table(const QkArgs& a, float2* tab, int b, int n0, int tokens) {
   const int p = threadIdx.x & ((1 << a.log_pairs) - 1);
   if (p >= a.pairs) return;
@@ -335,15 +336,16 @@ cudaError_t launch_norm(int norm, int rot, const QkArgs& a, dim3 grid, size_t sm
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
-// Frequencies of an axis's pairs in turns per position.  Powers by repeated multiplication, one call of pow() instead of one a pair
-// (1 us of a call's host time instead of 4): after i steps they are off by i / 2 units of 2^-52, but by then the frequency itself
-// has fallen so far that no angle is off by more than that of the first pairs.
+// Frequencies of an axis's pairs in turns per position, in long double (64 bits of fraction on x86: in double they alone turn position 2^31
+// by 2^-25).  Powers by repeated multiplication, one call of pow() instead of one a pair (0.7 us of host time for 64 pairs instead of 23; in double 0.6): pair i
+// is off by (2 i + 8) 2^-64 of its frequency at most, the fixed point by another 2^-64 of a turn.
 bool axis_frequencies(const vc_qk_params* p, int n, double factor, int original, double theta, uint64_t* out) {
   if (n == 0) return true;
   const int pairs = n / 2;
-  if (p->rope_scaling == VC_ROPE_SCALING_NTK && n > 2) theta *= std::pow(factor, (double)n / (n - 2));
-  if (!(theta > 0.0) || !std::isfinite(theta)) return false;
-  const double ratio = std::pow(theta, -2.0 / n);
+  long double base = theta;
+  if (p->rope_scaling == VC_ROPE_SCALING_NTK && n > 2) base *= std::pow((long double)factor, (long double)n / (n - 2));
+  if (!(base > 0) || !std::isfinite((double)base)) return false;
+  const long double ratio = std::pow(base, -2.0L / n);
   double lo = 0, hi = 1;
   if (p->rope_scaling == VC_ROPE_SCALING_YARN) {
     const double fast = p->yarn_beta_fast != 0.f ? p->yarn_beta_fast : 32.0, slow = p->yarn_beta_slow != 0.f ? p->yarn_beta_slow : 1.0;
@@ -354,16 +356,17 @@ bool axis_frequencies(const vc_qk_params* p, int n, double factor, int original,
     hi = hi < n - 1 ? hi : n - 1;
     if (hi - lo < 0.001) hi = lo + 0.001;
   }
-  double f = 1.0 / kTwoPi;
+  long double f = 0.159154943091895335768883763372514362L;      // 1 / (2 pi)
   for (int i = 0; i < pairs; ++i, f *= ratio) {
-    double v = f;
+    long double v = f;
     if (p->rope_scaling == VC_ROPE_SCALING_LINEAR) v /= factor;
     if (p->rope_scaling == VC_ROPE_SCALING_YARN) {
-      double r = (i - lo) / (hi - lo);
+      long double r = ((long double)i - lo) / ((long double)hi - lo);
       r = r < 0 ? 0 : (r > 1 ? 1 : r);
-      v = v * (1.0 - r) + v / factor * r;
+      v = v * (1 - r) + v / factor * r;
     }
-    out[i] = (uint64_t)std::ldexp(v - std::floor(v), 64);       // (below 2^64: v below 1 has 53 bits)
+    if (v >= 1) v -= std::floor(v);
+    out[i] = (uint64_t)(v * 18446744073709551616.0L);           // (2^64; exact, and below it: v is below 1)
   }
   return true;
 }

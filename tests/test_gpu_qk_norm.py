@@ -5,6 +5,9 @@ by 64 * 2^-24 of what the channel is a sum of: the sum of squares is a chain of 
 a thread, 5 shuffles and 16 partial sums (relative error below 90 * 2^-24 at the sizes here, halved by the root), then rsqrt
 (2 ulp), two multiplications, sincospi (its argument half an ulp of 1, which is pi * 2^-24, and 2 ulp), the factor, two products, one sum.
 """
+import math
+from decimal import Decimal, getcontext
+
 import numpy as np
 import pytest
 import torch
@@ -126,6 +129,48 @@ def test_positions_over_the_whole_range_of_int32(layout):
     pos[:, :4] = [[[-2 ** 31] * 3, [2 ** 31 - 1] * 3, [-1] * 3, [0] * 3]]
     _run(2, 2, 1, (300, 1, 1), 64, "bf16", "none", layout, (16, 32, 16), positions=pos)
     _run(1, 2, 1, (300, 1, 1), 64, "bf16", "head", layout, (16, 32, 16), start=(2 ** 31 - 400, 5, 2 ** 30))
+
+
+def _turns(positions, n, theta, scaling, factor):
+    """position * frequency of an axis's pairs in turns within [-1/2, 1/2], [positions, pairs], from 50 decimal digits."""
+    getcontext().prec = 50
+    two_pi, base, factor = 2 * Decimal("3.14159265358979323846264338327950288419716939937511"), Decimal(theta), Decimal(factor)
+    if scaling == "ntk":
+        base *= (factor.ln() * n / (n - 2)).exp()
+    out = np.empty((len(positions), n // 2))
+    for i in range(n // 2):
+        f = (base.ln() * -2 * i / n).exp() / two_pi / (factor if scaling == "linear" else 1)
+        out[:, i] = [float(int(p) * f - (int(p) * f).to_integral_value()) for p in positions]
+    return out
+
+
+@pytest.mark.parametrize("layout,dims", [(L.INTERLEAVED, (256, 0, 0)), (L.HALF, (256, 0, 0)), (L.HALF, (0, 0, 250))])
+@pytest.mark.parametrize("theta,scaling,factor", [(10000.0, "none", 1.0), (1.0009765625, "none", 1.0), (1.0 + 2.0 ** -23, "none", 1.0), (10000.0, "linear", 1.5),
+                                                  (1.0009765625, "ntk", 1.25)])
+def test_angles_of_the_farthest_positions(layout, dims, theta, scaling, factor):
+    """Frequencies that hardly fall from pair to pair, at positions up to 2^31, to the accuracy of FP32.
+
+    In units of 2^-24: the turns are off by 2^31 ((2 i + 8) f_i + 1) 2^-64 <= 44 * 2^-33 (0.6 in the angle), cut to 32 bits (0.03) and rounded to a float of at
+    most one half turn, 2^-25 of it (1.6); sincospi is off by 2 ulp of a value below 1 (2), a product by 1, the sum by 1: 6.2 of |a| + |b|, 8 with room."""
+    d, axis = 256, int(np.argmax(dims))
+    n = dims[axis]
+    rng = np.random.default_rng(21)
+    pos = np.zeros((1, 64, 3), np.int64)
+    pos[0, :, axis] = rng.integers(-2 ** 31, 2 ** 31, 64)
+    pos[0, :4, axis] = (-2 ** 31, 2 ** 31 - 1, -1, 10 ** 9)
+    x = torch.randn(1, 2, 64, d, generator=torch.Generator().manual_seed(22))
+    out = torch.empty(x.shape, device="cuda")
+    p = vc.QkParams.of(out, None, out, None, rotary=ROT[layout], rope_dims=dims, rope_theta=theta, rope_scaling=SCAL[scaling], rope_factor=(factor,) * 3)
+    vc.vc_qk_norm_rope(p, x.cuda(), None, None, None, torch.from_numpy(pos.astype(np.int32)).cuda(), out, None)
+    x, got = x.double().numpy(), out.double().cpu().numpy()
+    angle = 2.0 * math.pi * _turns(pos[0, :, axis], n, theta, scaling, factor)
+    for i in range(n // 2):
+        a, b = (2 * i, 2 * i + 1) if layout == L.INTERLEAVED else (i, i + n // 2)
+        c, s = np.cos(angle[:, i]), np.sin(angle[:, i])
+        tol = 8 * 2.0 ** -24 * (np.abs(x[..., a]) + np.abs(x[..., b]))
+        assert (np.abs(got[..., a] - (x[..., a] * c - x[..., b] * s)) <= tol).all(), i
+        assert (np.abs(got[..., b] - (x[..., a] * s + x[..., b] * c)) <= tol).all(), i
+    assert np.array_equal(got[..., n:], x[..., n:])
 
 
 @pytest.mark.parametrize("layout", [L.INTERLEAVED, L.HALF])
