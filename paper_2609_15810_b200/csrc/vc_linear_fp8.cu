@@ -45,6 +45,7 @@ struct LinearArgs {
   int M, N, blocks, tiles_b, splits, items;  // blocks: of 128 columns of K; tiles_b: tiles along B
   int out_dtype, bias_dtype;
   bool vec;                                  // rows of out start on 16-byte boundaries
+  bool copies;                               // and end on them: they leave by TMA
   bool joined;                               // the CTAs of a tile's splits are a cluster and join their sums themselves
   uint32_t limit, nonblocking;
 };
@@ -149,7 +150,8 @@ template <> __device__ __forceinline__ uint4 pack_chunk<__nv_bfloat16>(const flo
 template <> __device__ __forceinline__ uint4 pack_chunk<__half>(const float* f) {
   return make_uint4(pack16<__half>(f[0], f[1]), pack16<__half>(f[2], f[3]), pack16<__half>(f[4], f[5]), pack16<__half>(f[6], f[7]));
 }
-// The same as one copy of the warp's 32 rows at a time, where rows of `out` start on 16-byte boundaries; what lies outside of it the copy leaves out.
+// The same as one copy of the warp's 32 rows at a time, where rows of `out` start and end on 16-byte boundaries; what lies outside of it the copy
+// leaves out.  (It leaves out 16 bytes at a time: behind a row that ends in between it writes zeros up to the boundary.)
 template <typename O, int COLS>
 __device__ __forceinline__ void emit_copies(const float (&y)[COLS], uint32_t tile, const CUtensorMap* map, int col0, int row0, int rows, int lane) {
   using Out = attn::OutTile<64>;
@@ -434,16 +436,16 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constan
 #pragma unroll
           for (int i = 0; i < kCols; ++i) y[i] += __shfl_sync(0xffffffffu, mine[i / 32], i % 32);
         }
-        if (whole && a.vec) {
+        if (whole && a.copies) {
           if (a.out_dtype == VC_DTYPE_BF16) emit_copies<__nv_bfloat16, kCols>(y, tile, &tm_o, n0, row0, cols > 0 ? rows : 0, lane);
           else if (a.out_dtype == VC_DTYPE_FP16) emit_copies<__half, kCols>(y, tile, &tm_o, n0, row0, cols > 0 ? rows : 0, lane);
           else emit_copies<float, kCols>(y, tile, &tm_o, n0, row0, cols > 0 ? rows : 0, lane);
           continue;
         }
         if (!whole) emit_rows<float, kCols>(y, tile, a.part + ((int64_t)now.split * a.M + row0) * a.ldp + n0, a.ldp, rows, cols, true, lane);
-        else if (a.out_dtype == VC_DTYPE_BF16) emit_rows<__nv_bfloat16, kCols>(y, tile, static_cast<__nv_bfloat16*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, false, lane);
-        else if (a.out_dtype == VC_DTYPE_FP16) emit_rows<__half, kCols>(y, tile, static_cast<__half*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, false, lane);
-        else emit_rows<float, kCols>(y, tile, static_cast<float*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, false, lane);
+        else if (a.out_dtype == VC_DTYPE_BF16) emit_rows<__nv_bfloat16, kCols>(y, tile, static_cast<__nv_bfloat16*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
+        else if (a.out_dtype == VC_DTYPE_FP16) emit_rows<__half, kCols>(y, tile, static_cast<__half*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
+        else emit_rows<float, kCols>(y, tile, static_cast<float*>(a.out) + row0 * a.ldo + n0, a.ldo, rows, cols, a.vec, lane);
       }
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");       // the rows have left shared memory before the CTA may end
@@ -599,7 +601,7 @@ cudaError_t launch_linear(const vc_linear_params& r, const Plan& pl, const Linea
       !make_map8(&tb, SWAP ? x : w, SWAP ? r.M : r.N, r.K, SWAP ? r.ldx : r.ldw, C::kPair ? TN / 2 : TN))
     return cudaErrorUnknown;
   to = ta;                                   // (read where rows leave by copies alone)
-  if (!SWAP && a.vec && pl.splits == 1 && !make_map_out(&to, a.out, r)) return cudaErrorUnknown;
+  if (!SWAP && a.copies && pl.splits == 1 && !make_map_out(&to, a.out, r)) return cudaErrorUnknown;
   cudaError_t e = allow_smem<linear_fp8_kernel<SWAP, TN>>();
   if (e != cudaSuccess) return e;
   const int ctas = C::kPair ? 2 : pl.joined ? pl.splits : 1, room = sm_count() / (C::kPair ? 2 : 1);
@@ -646,6 +648,7 @@ extern "C" vc_status vc_linear_fp8(const vc_linear_params* p, const void* x_code
   a.M = r.M; a.N = r.N; a.blocks = pl.blocks; a.tiles_b = pl.tiles_b; a.splits = pl.splits; a.joined = pl.joined; a.items = (int)pl.items;
   a.out_dtype = r.out_dtype; a.bias_dtype = r.bias_dtype;
   a.vec = r.ldo * elem_size(r.out_dtype) % 16 == 0;
+  a.copies = a.vec && (int64_t)r.N * elem_size(r.out_dtype) % 16 == 0;
   a.limit = attn::attn_wait_limit();
   a.nonblocking = attn::attn_wait_nonblocking();
   cudaStream_t s = (cudaStream_t)stream;

@@ -163,6 +163,29 @@ def test_rows_of_wider_matrices_and_neighbours(M):
     assert (room[0] == 7).all() and (room[M + 1] == 7).all()
 
 
+@pytest.mark.parametrize("pitch", ["rows on 16 bytes", "odd rows"])
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("splits", [1, 3, 9])
+@pytest.mark.parametrize("M,N", [(1, 2500), (5, 2500), (50, 2499), (64, 130), (65, 2500), (200, 2499), (1301, 1801), (2500, 2500), (5000, 2003)])
+def test_what_lies_around_the_output_and_the_workspace_stays(M, N, splits, dt, pitch):
+    """Rows in front and behind, columns on both sides and the bytes around the workspace, for every shape of tile and way of joining parts."""
+    K, edge = 1168, 8 if dt == "bf16" else 4                        # ten blocks; elements of 16 bytes
+    x, xs, w, ws = _operands(M, N, K, 15)
+    wide = (N + 3 * edge) // edge * edge if pitch != "odd rows" else N + 2 * edge + 1 + N % 2
+    room = torch.full((M + 2 * edge, wide), -7.0, dtype=DT[dt], device="cuda")
+    out = room[edge:edge + M, edge:edge + N]
+    assert out.data_ptr() % 16 == 0 and (wide % edge == 0) == (pitch != "odd rows")
+    p = vc.LinearParams.of(_dev(x), _dev(w), out, None, k_splits=splits)
+    need = vc.vc_linear_workspace_bytes(p)
+    work = torch.full((need + 1024,), 0xa5, dtype=torch.uint8, device="cuda")
+    vc.vc_linear_fp8(p, _dev(x), _dev(xs), _dev(w), _dev(ws), None, out, work[512:512 + need])
+    vc.vc_poll_status(work[512:512 + need])
+    _close(out, x, xs, w, ws, dt)
+    out.fill_(-7.0)
+    assert (room == -7.0).all()
+    assert (work[:512] == 0xa5).all() and (work[512 + need:] == 0xa5).all()
+
+
 def test_scales_far_apart_and_zero():
     x, xs, w, ws = _operands(90, 140, 1024, 8, spread=6.0)
     xs[3], ws[0, 5] = 0.0, 0.0
