@@ -203,6 +203,55 @@ def test_nan_and_infinite_scales_stay_in_their_rows(M):
     assert torch.isnan(out[bad]).all() and torch.isfinite(out[~bad]).all()
 
 
+@pytest.mark.parametrize("M,N,splits", [(4, 150, 0), (50, 150, 3), (200, 300, 0), (200, 300, 4), (1301, 1801, 0)])
+def test_infinite_scales_make_infinities_and_nan_where_the_formula_does(M, N, splits):
+    """A sum over blocks with one that is infinite: the sign of that block's product, NaN where two of them disagree or the product is 0."""
+    K = 512
+    x, xs, w, ws = _operands(M, N, K, 16)
+    xs[1, 2], ws[1, 3] = np.inf, np.inf
+    x[3, 128:256] = 0                                               # (a product of 0 under a finite scale: nothing)
+    x[2, 300:] = 0
+    xs[0, 3] = np.inf
+    x[3, :128] = 0                                                  # under an infinite one: NaN
+    out = _run(_dev(x), _dev(xs), _dev(w), _dev(ws), "fp32", k_splits=splits).double().cpu().numpy()
+    val, want, sure = L.e4m3_values(), np.zeros((M, N)), np.ones((M, N), bool)
+    with np.errstate(invalid="ignore"):
+        for kb in range(K // 128):
+            part = slice(128 * kb, 128 * kb + 128)
+            a, b = val[x[:, part]], val[w[:, part]]
+            S, size = a @ b.T, np.abs(a) @ np.abs(b).T
+            f = xs[kb][:, None].astype(np.float64) * np.repeat(ws[:, kb].astype(np.float64), 128)[None, :N]
+            want += f * S
+            sure &= np.isfinite(f) | (size == 0) | (np.abs(S) > 132 * 2.0 ** -24 * size)      # (else its sign is a matter of rounding)
+    odd = ~np.isfinite(want)
+    assert odd[2].all() and np.isnan(want[3]).all() and odd[:, 128:256].all() and odd.sum() == 2 * N + (M - 2) * min(N - 128, 128)
+    assert sure.mean() > 0.99 and not np.isfinite(out[odd]).any() and np.isfinite(out[~odd]).all()
+    assert np.array_equal(out[odd & sure], want[odd & sure], equal_nan=True)
+    keep = ~odd.any(axis=1)
+    assert not keep.any()
+    few = [m for m in range(M) if m not in (2, 3)]
+    _close(torch.from_numpy(out[few][:, :128]), x[few], xs[:, few], w[:128], ws[:1], "fp32")
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("M", [4, 300])
+def test_quantised_infinities_and_nan_become_nan(M, bad):
+    """The blocks that hold one stand for NaN throughout: their row of y, and the 128 columns of their weights."""
+    g = torch.Generator().manual_seed(17)
+    x, w = torch.randn(M, 400, generator=g).cuda(), torch.randn(300, 400, generator=g).cuda()
+    x[1, 390], w[140, 5] = bad, bad
+    args = []
+    for t, rows in ((x, 1), (w, 128)):
+        codes = torch.empty(t.shape, dtype=torch.float8_e4m3fn, device="cuda")
+        scale = torch.empty((4, M) if rows == 1 else (3, 4), device="cuda")
+        vc.vc_quant_fp8(vc.QuantParams.of(t, rows), t, codes, scale)
+        args += [codes, scale]
+    out = _run(*args, "fp32").cpu()
+    bad = torch.zeros(M, 300, dtype=torch.bool)
+    bad[1], bad[:, 128:256] = True, True
+    assert torch.isnan(out[bad]).all() and torch.isfinite(out[~bad]).all()
+
+
 def test_codes_as_quantised_and_as_float8_tensors():
     """Quantised by the library and multiplied: the product of what the codes stand for."""
     g = torch.Generator().manual_seed(10)
