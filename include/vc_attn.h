@@ -442,7 +442,9 @@ vc_status vc_quant_fp8(const vc_quant_params *p, const void *x, void *codes, flo
  *
  *   y[m][n] = sum over blocks kb of x_scale[kb][m] w_scale[n / 128][kb] (sum of x[m][k] w[n][k] over k in block kb) + bias[n]
  *
- * Products are exact, sums FP32, one rounding to out_dtype.  x_codes [M][K] with block_rows = 1, w_codes [N][K] with
+ * Products are exact, sums FP32, one rounding to out_dtype.  x_scale w_scale is formed first, in FP32: it is to be 0 or from 2^-126 up to
+ * below 2^128 (below, it loses bits; above, it is infinite).  Those of vc_quant_fp8 are, where the two blocks' amax multiply to 2^-108 or
+ * more, or one of them is all zeros.  x_codes [M][K] with block_rows = 1, w_codes [N][K] with
  * block_rows = 128, rows ldx / ldw bytes apart (multiples of 16; 0 = K); out [M][N], rows ldo elements apart (0 = N); bias [N]
  * or NULL.  Few rows: the sum over K is split between CTAs and joined in a fixed order (k_splits = 1 forbids it,
  * 0 leaves the number to the library).  workspace: as for vc_cross_attn, vc_linear_workspace_bytes(p) bytes. */

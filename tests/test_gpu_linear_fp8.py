@@ -252,6 +252,26 @@ def test_quantised_infinities_and_nan_become_nan(M, bad):
     assert torch.isnan(out[bad]).all() and torch.isfinite(out[~bad]).all()
 
 
+@pytest.mark.parametrize("M,N,splits", [(1, 300, 0), (7, 300, 3), (50, 300, 9), (200, 300, 0), (1301, 1801, 0)])
+@pytest.mark.parametrize("x_exp,w_exp,dim", [(-61, -61, False), (-22, -100, False), (-100, -22, False), (-120, -2, False), (61, 61, True), (118, 4, True)])
+def test_products_of_scales_near_the_ends_of_the_range_of_fp32(M, N, splits, x_exp, w_exp, dim):
+    """x_scale * w_scale from 2^-126 and up to 2^127, as far as they are to be used: no bits are lost on the way."""
+    K = 1168
+    x, xs, w, ws = _operands(M, N, K, 18, spread=0.3)
+    if dim:
+        x, w = (c & 0x83 for c in (x, w))                           # magnitudes below 2^-6: products below 2^-12, sums of ten blocks below 2^-2
+        x[x & 127 == 0] |= 1
+    xs, ws = np.ldexp(xs, x_exp).astype(np.float32), np.ldexp(ws, w_exp).astype(np.float32)
+    f = [t.astype(np.float64) for t in (xs, ws)]
+    assert all(2.0 ** -126 <= f[0][kb].min() * f[1][:, kb].min() and f[0][kb].max() * f[1][:, kb].max() < 2.0 ** 127 for kb in range(K // 128 + 1))
+    out = _run(_dev(x), _dev(xs), _dev(w), _dev(ws), "fp32", k_splits=splits).cpu().double().numpy()
+    want, size = L.linear_fp8(x, xs, w, ws)
+    assert np.isfinite(want).all() and 2.0 ** -126 < np.median(np.abs(want)) and np.abs(want).max() < 2.0 ** 128
+    # as above; and each block's term, and each of their sums, may lie on the grid of the subnormals: half a step of 2^-149 each
+    tol = (132 + 10 + 8) * 2.0 ** -24 * size + 2.0 ** -24 * np.abs(want) + 20 * 2.0 ** -150
+    assert (np.abs(out - want) <= tol).all(), np.nanmax(np.abs(out - want) / tol)
+
+
 def test_codes_as_quantised_and_as_float8_tensors():
     """Quantised by the library and multiplied: the product of what the codes stand for."""
     g = torch.Generator().manual_seed(10)
