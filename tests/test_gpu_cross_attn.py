@@ -258,6 +258,29 @@ def test_layouts_views_and_neighbours():
         assert (room[:, 0] == 7).all() and (room[:, N + 1] == 7).all() and (room[..., d:] == 7).all()
 
 
+@pytest.mark.parametrize("dt,d", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nkv,splits", [(2, 45, 45, 300, 130, 1), (2, 45, 9, 300, 300, 2), (2, 3, 1, 129, 700, 1), (1, 4, 2, 5, 4096, 0), (1, 4, 2, 100, 2048, 4),
+                                                   (1, 2, 2, 131, 1300, 9), (2, 2, 2, 1, 0, 0)])
+def test_what_lies_around_the_outputs_and_the_workspace_stays(dt, d, B, H, Hkv, Nq, Nkv, splits):
+    """One and two query tiles an item, parts joined by a cluster and by a launch, no keys; a batch without any."""
+    g = torch.Generator().manual_seed(Nq + Nkv)
+    q, k, v = _heads(B, H, Nq, d, dt, g), _heads(B, Hkv, Nkv, d, dt, g), _heads(B, Hkv, Nkv, d, dt, g)
+    lens = torch.tensor([Nkv, 0][:B], dtype=torch.int32, device="cuda")
+    room = torch.full((B + 2, Nq + 2, H + 2, d + 8), 7.0, dtype=DT[dt], device="cuda")
+    o = room[1:B + 1, 1:Nq + 1, 1:H + 1, :d].transpose(1, 2)
+    lse = torch.full((B * H * Nq + 8,), 7.0, device="cuda")
+    p = vc.CrossParams.of(q, k, v, o, key_splits=splits)
+    need = vc.vc_cross_workspace_bytes(p)
+    work = torch.full((need + 1024,), 0xa5, dtype=torch.uint8, device="cuda")
+    mine = lse[4:-4].view(B, H, Nq)
+    vc.vc_cross_attn(p, q, k, v, lens, None, o, mine, work[512:512 + need])
+    vc.vc_poll_status(work[512:512 + need])
+    _check(q, k, v, o, mine, lens)
+    o.fill_(7.0)
+    assert (room == 7).all() and (lse[:4] == 7).all() and (lse[-4:] == 7).all()
+    assert (work[:512] == 0xa5).all() and (work[512 + need:] == 0xa5).all()
+
+
 def test_broadcast_keys_and_queries():
     g = torch.Generator().manual_seed(27)
     q1, k1, v1 = _heads(1, 1, 70, 64, "bf16", g), _heads(1, 2, 200, 64, "bf16", g), _heads(3, 1, 200, 64, "bf16", g)
