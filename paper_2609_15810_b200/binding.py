@@ -437,7 +437,7 @@ def _address(t, device, want):
         raise ValueError(f"{name}: {t.dtype}, not {' or '.join(str(d) for d in types)}")
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, not {shape}")
-    if t.stride() != strides:          # (a dimension of one entry may have any)
+    if t.stride() != strides and 0 not in shape:          # (a dimension of one entry may have any, a tensor without entries too)
         for n, got, wanted in zip(shape, t.stride(), strides):
             if n > 1 and got != wanted:
                 raise ValueError(f"{name}: strides {t.stride()}, not {strides}")

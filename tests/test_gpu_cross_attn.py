@@ -243,6 +243,14 @@ def test_no_keys_at_all():
     assert (o == 0).all() and torch.isneginf(lse).all()
 
 
+@pytest.mark.parametrize("mask_type", [torch.bool, torch.uint8])
+def test_no_keys_under_a_mask_and_lengths(mask_type):
+    q = torch.randn(3, 4, 150, 64, device="cuda").bfloat16()
+    k = torch.empty(3, 0, 2, 64, device="cuda", dtype=torch.bfloat16).transpose(1, 2)
+    o, lse = _call(q, k, k, torch.tensor([0, 3, -1], dtype=torch.int32, device="cuda"), torch.empty(3, 0, dtype=mask_type, device="cuda"))
+    assert (o == 0).all() and torch.isneginf(lse).all()
+
+
 def test_layouts_views_and_neighbours():
     """Queries and outputs inside [B, N, H, d] memory, keys and values two halves of one projection; what lies around the output stays."""
     g = torch.Generator().manual_seed(26)

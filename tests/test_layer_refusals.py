@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2609_15810_b200 as vc
+from paper_2609_15810_b200 import binding
 from paper_2609_15810_b200.binding import CrossParams, LinearParams, QkParams, QuantParams, Strides
 
 P = 4096          # stands for an aligned address: a refused call never looks at it
@@ -207,3 +208,14 @@ def test_sizes_of_the_parameter_blocks():
     assert ctypes.sizeof(CrossParams) == 8 * 4 + 4 + 4 + 4 * 24          # 4 bytes of padding in front of the strides, as in C
     assert ctypes.sizeof(LinearParams) == 6 * 4 + 3 * 8
     assert ctypes.sizeof(QuantParams) == 6 * 4 + 24
+
+
+def test_a_key_mask_of_no_keys_is_taken():
+    """[B, 0] tensors have strides of their own; with nothing to address none is wrong."""
+    p = CrossParams(B=3, H=4, H_kv=2, N_q=5, N_kv=0, d=64)
+    want = binding._cross_wants(p)[4]
+    for dt in (torch.bool, torch.uint8):
+        binding._address(torch.zeros(3, 0, dtype=dt), -1, want)
+    for wrong in (torch.zeros(2, 0, dtype=torch.bool), torch.zeros(3, 1, dtype=torch.bool), torch.zeros(3, 0)):
+        with pytest.raises(ValueError):
+            binding._address(wrong, -1, want)
