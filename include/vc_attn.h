@@ -395,6 +395,12 @@ typedef struct {
 vc_status vc_qk_norm_rope(const vc_qk_params *p, const void *q, const void *k, const void *q_weight,
                           const void *k_weight, const int32_t *positions, void *q_out, void *k_out, void *stream);
 
+/* The same with theta and the axes' factors in 64 bits, each in the place of the field of vc_qk_params unless it is 0; `rope` (host
+ * memory, read during the call) may be NULL.  As fields they are FP32: one that FP32 does not hold turns an angle of 10^5 by up to 0.006. */
+typedef struct { double theta, factor_t, factor_h, factor_w; } vc_rope_values;
+vc_status vc_qk_norm_rope_with_values(const vc_qk_params *p, const vc_rope_values *rope, const void *q, const void *k, const void *q_weight,
+                                      const void *k_weight, const int32_t *positions, void *q_out, void *k_out, void *stream);
+
 /* Attention of N_q queries to the N_kv states of an encoder, per (b, h):
  *
  *   o = softmax(softmax_scale q k^T over the kept keys) v        lse = ln sum exp(softmax_scale q k^T)

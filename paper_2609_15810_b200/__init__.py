@@ -14,7 +14,7 @@ from .binding import (VcError, Params, QuantView, load_library, vc_attn, vc_attn
                       VC_FLAG_ALL, VC_FLAG_HADAMARD, VC_FLAG_INT8_QK, VC_FLAG_K_SMOOTH, VC_FLAG_ROPE, VC_FLAG_V_SMOOTH,
                       VC_P_DEFAULT, VC_P_EXPCAST_E4M3, VC_P_EXP_E4M3, VC_P_NVFP4,
                       VC_P_EXP_POLY_E4M3, VC_P_EXP_MIX_E4M3,
-                      CrossParams, LinearParams, QkParams, QuantParams, vc_cross_attn, vc_cross_workspace_bytes, vc_linear_fp8,
+                      CrossParams, LinearParams, QkParams, QuantParams, RopeValues, vc_cross_attn, vc_cross_workspace_bytes, vc_linear_fp8,
                       vc_linear_workspace_bytes, vc_qk_norm_rope, vc_quant_fp8, VC_DTYPE_BF16, VC_DTYPE_FP16, VC_DTYPE_FP32,
                       VC_NORM_NONE, VC_NORM_HEAD, VC_NORM_TOKEN, VC_ROTARY_NONE, VC_ROTARY_INTERLEAVED, VC_ROTARY_HALF,
                       VC_ROPE_SCALING_NONE, VC_ROPE_SCALING_LINEAR, VC_ROPE_SCALING_NTK, VC_ROPE_SCALING_YARN)

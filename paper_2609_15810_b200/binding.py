@@ -89,8 +89,14 @@ class Strides(ctypes.Structure):
         return cls(t.stride(0), t.stride(1), t.stride(2) or t.shape[3])         # (all zero would mean packed)
 
 
+class RopeValues(ctypes.Structure):
+    """Mirror of vc_rope_values."""
+    _fields_ = [(n, ctypes.c_double) for n in ("theta", "factor_t", "factor_h", "factor_w")]
+
+
 class QkParams(ctypes.Structure):
-    """Mirror of vc_qk_params."""
+    """Mirror of vc_qk_params.  `rope` is None, or a RopeValues to go with the block: `of` makes one where theta or a factor is no FP32 number."""
+    rope = None
     _fields_ = ([(n, ctypes.c_int32) for n in ("B", "N", "d", "H_q", "H_k", "dtype", "weight_dtype", "norm", "rotary",
                                                "rope_dim_t", "rope_dim_h", "rope_dim_w", "grid_t", "grid_h", "grid_w",
                                                "start_t", "start_h", "start_w", "rope_scaling",
@@ -119,7 +125,26 @@ class QkParams(ctypes.Structure):
                 setattr(p, f"{field}_{axis}", v)
         for name, v in kw.items():
             setattr(p, name, v)
+        exact = (float(kw.get("rope_theta", 0.0)), *map(float, rope_factor[:3]))
+        if exact != p.rope_fields():
+            p.rope = RopeValues(*exact)
+            p.rope_rounded = p.rope_fields()
         return p
+
+    def rope_fields(self):
+        return self.rope_theta, self.rope_factor_t, self.rope_factor_h, self.rope_factor_w
+
+    def rope_values(self):
+        """The address of what goes with the block, or None; a field changed since `of` stands."""
+        if self.rope is None:
+            return None
+        fields, rounded = self.rope_fields(), getattr(self, "rope_rounded", None)
+        if rounded is not None and fields != rounded:
+            for (name, _), field, was in zip(RopeValues._fields_, fields, rounded):
+                if field != was:
+                    setattr(self.rope, name, 0.0)
+            self.rope_rounded = fields
+        return ctypes.addressof(self.rope)
 
 
 class CrossParams(ctypes.Structure):
@@ -220,6 +245,8 @@ def load_library():
                                 ctypes.POINTER(ctypes.c_double), vp]
     lib.vc_qk_norm_rope.restype = ctypes.c_int
     lib.vc_qk_norm_rope.argtypes = [ctypes.POINTER(QkParams)] + [vp] * 8
+    lib.vc_qk_norm_rope_with_values.restype = ctypes.c_int
+    lib.vc_qk_norm_rope_with_values.argtypes = [ctypes.POINTER(QkParams)] + [vp] * 9
     lib.vc_cross_workspace_bytes.restype = ctypes.c_size_t
     lib.vc_cross_workspace_bytes.argtypes = [ctypes.POINTER(CrossParams)]
     lib.vc_cross_attn.restype = ctypes.c_int
@@ -467,9 +494,9 @@ def _qk_wants(p):
 def vc_qk_norm_rope(p, q, k, q_weight, k_weight, positions, q_out, k_out):
     """RMS norm (p.norm) and rotation (p.rotary) of q and k into q_out and k_out; q, k, a weight [d] or [H d], or positions may be None."""
     dev, w = torch.cuda.current_device(), _wanted(p, _qk_wants)
-    _check(load_library().vc_qk_norm_rope(ctypes.byref(p), _address(q, dev, w[0]), _address(k, dev, w[1]), _address(q_weight, dev, w[2]),
-                                          _address(k_weight, dev, w[3]), _address(positions, dev, w[4]), _address(q_out, dev, w[5]),
-                                          _address(k_out, dev, w[6]), _stream()), "vc_qk_norm_rope")
+    _check(load_library().vc_qk_norm_rope_with_values(ctypes.byref(p), p.rope_values(), _address(q, dev, w[0]), _address(k, dev, w[1]),
+                                                      _address(q_weight, dev, w[2]), _address(k_weight, dev, w[3]), _address(positions, dev, w[4]),
+                                                      _address(q_out, dev, w[5]), _address(k_out, dev, w[6]), _stream()), "vc_qk_norm_rope")
 
 
 def vc_cross_workspace_bytes(p):

@@ -371,15 +371,10 @@ bool axis_frequencies(const vc_qk_params* p, int n, double factor, int original,
   return true;
 }
 
-bool not_positive(float v) { return v != 0.f && !(v > 0.f && std::isfinite(v)); }
+bool not_positive(double v) { return v != 0.0 && !(v > 0.0 && std::isfinite(v)); }
 
-}  // namespace
-}  // namespace vc
-
-using namespace vc;
-
-extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const void* k, const void* q_weight,
-                                     const void* k_weight, const int32_t* positions, void* q_out, void* k_out, void* stream) {
+vc_status qk_norm_rope(const vc_qk_params* p, const vc_rope_values& rope, const void* q, const void* k, const void* q_weight, const void* k_weight,
+                       const int32_t* positions, void* q_out, void* k_out, void* stream) {
   if (!p) return VC_ERR_INVALID_ARG;
   if (p->B < 1 || p->B > 65535 || p->N < 1 || p->N > (1 << 22)) return VC_ERR_INVALID_ARG;
   if (p->d < 8 || p->d > 256 || p->d % 8) return VC_ERR_INVALID_ARG;
@@ -407,9 +402,9 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
   if (rot != VC_ROTARY_NONE) {
     int dims[3] = {p->rope_dim_t, p->rope_dim_h, p->rope_dim_w};
     if (!dims[0] && !dims[1] && !dims[2]) { dims[1] = dims[2] = 2 * (p->d / 6); dims[0] = p->d - 2 * dims[1]; }
-    const float factors[3] = {p->rope_factor_t, p->rope_factor_h, p->rope_factor_w};
+    const double factors[3] = {rope.factor_t, rope.factor_h, rope.factor_w};
     const int original[3] = {p->rope_original_t, p->rope_original_h, p->rope_original_w};
-    const double theta = p->rope_theta != 0.f ? p->rope_theta : 10000.0;
+    const double theta = rope.theta != 0.0 ? rope.theta : 10000.0;
     if (!(theta > 1.0) || !std::isfinite(theta)) return VC_ERR_INVALID_ARG;
     if (p->rope_scaling < VC_ROPE_SCALING_NONE || p->rope_scaling > VC_ROPE_SCALING_YARN) return VC_ERR_INVALID_ARG;
     if (not_positive(p->yarn_beta_fast) || not_positive(p->yarn_beta_slow) || not_positive(p->rope_attention_factor)) return VC_ERR_INVALID_ARG;
@@ -418,7 +413,7 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
     for (int i = 0; i < 3; ++i) {
       if (dims[i] < 0 || dims[i] % 2 || dims[i] > p->d || not_positive(factors[i])) return VC_ERR_INVALID_ARG;
       if (2 * pairs + dims[i] > p->d) return VC_ERR_INVALID_ARG;
-      const double factor = factors[i] != 0.f ? factors[i] : 1.0;
+      const double factor = factors[i] != 0.0 ? factors[i] : 1.0;
       if (dims[i] && p->rope_scaling == VC_ROPE_SCALING_YARN && original[i] < 1) return VC_ERR_INVALID_ARG;
       if (!axis_frequencies(p, dims[i], factor, original[i], theta, a.turns + pairs)) return VC_ERR_INVALID_ARG;
       if (dims[i] && factor > largest) largest = factor;
@@ -495,4 +490,27 @@ extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const
   if (e != cudaSuccess) return VC_ERR_CUDA;
   count_launches(1);
   return VC_OK;
+}
+
+}  // namespace
+}  // namespace vc
+
+using namespace vc;
+
+extern "C" vc_status vc_qk_norm_rope_with_values(const vc_qk_params* p, const vc_rope_values* rope, const void* q, const void* k, const void* q_weight,
+                                                 const void* k_weight, const int32_t* positions, void* q_out, void* k_out, void* stream) {
+  if (!p) return VC_ERR_INVALID_ARG;
+  vc_rope_values v = {p->rope_theta, p->rope_factor_t, p->rope_factor_h, p->rope_factor_w};
+  if (rope) {
+    if (rope->theta != 0.0) v.theta = rope->theta;
+    if (rope->factor_t != 0.0) v.factor_t = rope->factor_t;
+    if (rope->factor_h != 0.0) v.factor_h = rope->factor_h;
+    if (rope->factor_w != 0.0) v.factor_w = rope->factor_w;
+  }
+  return qk_norm_rope(p, v, q, k, q_weight, k_weight, positions, q_out, k_out, stream);
+}
+
+extern "C" vc_status vc_qk_norm_rope(const vc_qk_params* p, const void* q, const void* k, const void* q_weight,
+                                     const void* k_weight, const int32_t* positions, void* q_out, void* k_out, void* stream) {
+  return vc_qk_norm_rope_with_values(p, nullptr, q, k, q_weight, k_weight, positions, q_out, k_out, stream);
 }

@@ -140,15 +140,21 @@ def _turns(positions, n, theta, scaling, factor):
     out = np.empty((len(positions), n // 2))
     for i in range(n // 2):
         f = (base.ln() * -2 * i / n).exp() / two_pi / (factor if scaling == "linear" else 1)
+        if scaling == "yarn":
+            lo, hi = (n * math.log(4096 / (2 * math.pi * b)) / (2 * math.log(theta)) for b in (32.0, 1.0))
+            lo, hi = max(math.floor(lo), 0), min(math.ceil(hi), n - 1)
+            r = min(max(Decimal(i - lo) / Decimal(hi - lo), Decimal(0)), Decimal(1))
+            f = f * (1 - r) + f / factor * r
         out[:, i] = [float(int(p) * f - (int(p) * f).to_integral_value()) for p in positions]
     return out
 
 
 @pytest.mark.parametrize("layout,dims", [(L.INTERLEAVED, (256, 0, 0)), (L.HALF, (256, 0, 0)), (L.HALF, (0, 0, 250))])
 @pytest.mark.parametrize("theta,scaling,factor", [(10000.0, "none", 1.0), (1.0009765625, "none", 1.0), (1.0 + 2.0 ** -23, "none", 1.0), (10000.0, "linear", 1.5),
-                                                  (1.0009765625, "ntk", 1.25)])
+                                                  (1.0009765625, "ntk", 1.25), (12345.678, "none", 1.0), (10000.0, "linear", 3.3), (12345.678, "ntk", 2.7),
+                                                  (10000.0, "yarn", 1.1)])
 def test_angles_of_the_farthest_positions(layout, dims, theta, scaling, factor):
-    """Frequencies that hardly fall from pair to pair, at positions up to 2^31, to the accuracy of FP32.
+    """Frequencies that hardly fall from pair to pair, theta and factors that are no FP32 numbers, at positions up to 2^31, to the accuracy of FP32.
 
     In units of 2^-24: the turns are off by 2^31 ((2 i + 8) f_i + 1) 2^-64 <= 44 * 2^-33 (0.6 in the angle), cut to 32 bits (0.03) and rounded to a float of at
     most one half turn, 2^-25 of it (1.6); sincospi is off by 2 ulp of a value below 1 (2), a product by 1, the sum by 1: 6.2 of |a| + |b|, 8 with room."""
@@ -160,7 +166,8 @@ def test_angles_of_the_farthest_positions(layout, dims, theta, scaling, factor):
     pos[0, :4, axis] = (-2 ** 31, 2 ** 31 - 1, -1, 10 ** 9)
     x = torch.randn(1, 2, 64, d, generator=torch.Generator().manual_seed(22))
     out = torch.empty(x.shape, device="cuda")
-    p = vc.QkParams.of(out, None, out, None, rotary=ROT[layout], rope_dims=dims, rope_theta=theta, rope_scaling=SCAL[scaling], rope_factor=(factor,) * 3)
+    p = vc.QkParams.of(out, None, out, None, rotary=ROT[layout], rope_dims=dims, rope_theta=theta, rope_scaling=SCAL[scaling], rope_factor=(factor,) * 3,
+                       rope_original=(4096,) * 3, rope_attention_factor=1.0)
     vc.vc_qk_norm_rope(p, x.cuda(), None, None, None, torch.from_numpy(pos.astype(np.int32)).cuda(), out, None)
     x, got = x.double().numpy(), out.double().cpu().numpy()
     angle = 2.0 * math.pi * _turns(pos[0, :, axis], n, theta, scaling, factor)

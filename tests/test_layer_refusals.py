@@ -49,6 +49,34 @@ def test_qk_norm_rope_in_place_wants_the_same_strides():
     assert _qk(ptrs=(P, P, P, P, None, P, 2 * P), q_out=Strides(0, 64, 128)) == vc.VC_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("values", [(0.5, 0, 0, 0), (1.0, 0, 0, 0), (float("inf"), 0, 0, 0), (float("nan"), 0, 0, 0), (0, -1.5, 0, 0), (0, 0, float("nan"), 0),
+                                    (0, 0, 0, float("inf"))])
+def test_qk_norm_rope_values(values):
+    p = QkParams(B=1, N=24, d=64, H_q=2, H_k=2, grid_t=2, grid_h=3, grid_w=4, norm=vc.VC_NORM_HEAD, rotary=vc.VC_ROTARY_HALF, rope_scaling=vc.VC_ROPE_SCALING_LINEAR)
+    rope = vc.RopeValues(*values)
+    assert vc.load_library().vc_qk_norm_rope_with_values(ctypes.byref(p), ctypes.byref(rope), *NO_POS, None) == vc.VC_ERR_INVALID_ARG
+    assert vc.load_library().vc_qk_norm_rope_with_values(None, ctypes.byref(rope), *NO_POS, None) == vc.VC_ERR_INVALID_ARG
+    p.rope_theta = 0.5                                            # (without values the fields are looked at)
+    assert vc.load_library().vc_qk_norm_rope_with_values(ctypes.byref(p), None, *NO_POS, None) == vc.VC_ERR_INVALID_ARG
+
+
+def test_theta_and_factors_keep_their_64_bits_on_the_way():
+    x = torch.zeros(1, 2, 24, 64)
+    of = lambda **kw: QkParams.of(x, None, x, None, grid=(2, 3, 4), **kw)
+    for p in (of(), of(rope_theta=10000.0, rope_factor=(4.0, 1.5, 0.0))):
+        assert p.rope is None and p.rope_values() is None
+    p = of(rope_theta=12345.678, rope_factor=(3.3, 2.0, 0.1))
+    at = p.rope_values()
+    got = vc.RopeValues.from_address(at)
+    assert (got.theta, got.factor_t, got.factor_h, got.factor_w) == (12345.678, 3.3, 2.0, 0.1) and abs(p.rope_factor_t - 3.3) < 1e-6
+    p.rope_factor_t = 8.0                                         # a field that is changed stands, the others keep theirs
+    p.rope_theta = 0.0
+    got = vc.RopeValues.from_address(p.rope_values())
+    assert (got.theta, got.factor_t, got.factor_h, got.factor_w) == (0.0, 0.0, 2.0, 0.1) and p.rope_factor_t == 8.0
+    assert p.rope_values() == ctypes.addressof(p.rope)
+    assert ctypes.sizeof(vc.RopeValues) == 32
+
+
 OVERLAPPING = [Strides(0, 8, 64), Strides(0, 64, 64), Strides(0, 64, 72), Strides(0, 64 * 23, 64), Strides(0, 128, 64)]
 
 
