@@ -5,7 +5,9 @@
 // 8-11 are the softmax of the two query tiles, 12-15 the epilogue.
 //
 //   S_t = Q_t K^T    both operands in shared memory, K-major, FP32 accumulators in 128 columns of tensor memory
-//   P_t = 2^(s S_t - m)  in registers, a thread a row; written back as 16-bit values over S_t's own columns
+//   P_t = 2^(s S_t - m)  in registers, a thread a row; written back as 16-bit values over S_t's own columns: both operands of a product have
+//                        one type, and P in two parts would double the second product.  (Error against 64 bits in bf16 0.0022 of the outputs' 2-norm,
+//                        where rounding the outputs alone gives 0.0017; fp16 0.00024 and 0.00021.)
 //   O_t += P_t V     P_t from tensor memory, V as it was loaded ([key][channel], read MN-major)
 //
 // The running maximum m of a row is a reference, not the exact maximum: O_t and the row sum are rescaled only when a tile
@@ -14,8 +16,10 @@
 // issued in front of it, is complete too.
 //
 // What bounds it: per query tile the chain S_t -> softmax (1900 cycles) -> O_t product and next S_t (1024 at d = 128, 1300 with the
-// hand-overs), two of which overlap; a pair of tiles of 128 keys takes 3500 cycles, where the tensor cores need
-// 2048.  B1 H40 32760 x 512 d128 320 us (1075 TFLOP/s), 8192 x 4096 577 us (1190).  Tried and slower there: one warp that issues
+// hand-overs), two of which overlap; a pair of query tiles takes 3550 cycles for 128 keys, where the tensor cores need
+// 2048 and the exponentials as many, and an item's ends take 1300 more (512 keys 15510 an item, 128 keys 6440: there nothing covers them).  B1 H40 32760 x 512
+// d128 is 556000 cycles at any clock: 320-340 us in the first ten calls (1.65 GHz; 1010 to 1075 TFLOP/s), 365-395 behind hundreds (1.4 to 1.5 GHz, the
+// power cap); 8192 x 4096 577-605 and 660; 32760 x 512 d64 280-292 in both.  Tried and slower there (first calls): one warp that issues
 // for both tiles 332 us (its waits and descriptors lie between the products; 567 at 4096 keys), two that do not take turns (both tiles in the same phase),
 // the turn passed at half of a tile's scores 344, two threads a row and 24 warps 358, a polynomial for one exponential in 8 / 4 / 3: 344 / 360 / 372,
 // scores read twice from tensor memory instead of held in registers 363 (650 at 4096), the second half of P handed over on its own 343,
@@ -700,6 +704,7 @@ vc_status resolve(const vc_cross_params* p, vc_cross_params* out, Plan* plan) {
   pl.items = bh * pl.qitems * pl.splits;
   if (pl.items > INT32_MAX) return VC_ERR_UNSUPPORTED;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  // (The parts have their place also where a cluster joins them in shared memory: the size goes by the splits alone.)
   pl.part_o = 256;
   pl.part_lse = pl.part_o + (pl.splits > 1 ? up((size_t)pl.splits * pl.rows * r.d * 4) : 0);
   pl.total = pl.part_lse + (pl.splits > 1 ? up((size_t)pl.splits * pl.rows * 4) : 0);

@@ -13,16 +13,19 @@
 // fewer tiles than SMs the blocks of K are split between CTAs and the parts joined in a fixed order: up to 64 rows by a cluster of the CTAs, from shared
 // memory, else by a second launch.
 //
-// What bounds the large ones: per block the tensor cores need 512 cycles, 128 x 256 sums out of tensor memory 256 and their additions
-// 256 of the FMA pipe, side by side; but there are two buffers only (256 columns each of 512), and a buffer's round, product 512, signal 100,
-// read and additions 450, signal 150, takes longer than two products.  32760 x 5120 x 5120 735 us in single calls at 1965 MHz, 805 one
-// behind the other under the power cap (1500 MHz).  A CTA by itself on 128 x 256 (48 KB copied and 48 KB read per block and 512 cycles
-// from a shared memory that gives 128 bytes a cycle): 808 and 880.  One issuing warp instead of two that take every other block (a group of products
-// begins 150 cycles behind the end of the one in front if the same warp issued it): 781, and the same under the cap.  Four buffers of
-// 128 columns (two products of 256 x 128 a block, A read twice): 794, and 868 under the cap.  A release or acquire of
-// cluster scope at the buffers' barriers: 1490 (it waits for every load in flight).  Packed additions: 860 (a move and a half each, the products
-// arrive in registers that do not pair up).  Four warpgroups of 64 columns, scales four blocks ahead: no gain.
-// 5120 x 5120 with weights in L2: one row 7.7 us (26 MB at the copy rate 4.0), 512 rows 22, 1024 rows 40.
+// What bounds the large ones: a block takes 836 cycles, at any clock (clock reads around the waits in a scratch build): an adding warp reads and adds
+// for 505 of them and waits 221 for the product, a tile's end comes to 110 (4400 a tile of 40 blocks).  The tensor cores need 512, but there are two buffers
+// only (256 columns each of 512): an issuing warp waits for its buffer to be free for half of its time, 844 of 1670 cycles a buffer.
+// 32760 x 5120 x 5120 is 1.175e6 cycles: 726-743 us in the first ten calls (1.6 GHz), 840-855 behind a hundred (1.38 GHz, the power cap).
+// Tried (first calls / behind many): a CTA by itself on 128 x 256 (48 KB copied and 48 KB read per block and 512 cycles
+// from a shared memory that gives 128 bytes a cycle) 808 / 880 us; one issuing warp instead of two that take every other block (a group of products
+// begins 150 cycles behind the end of the one in front if the same warp issued it) 781, and the same under the cap; four buffers of
+// 128 columns (two products of 256 x 128 a block, A read twice) 794 / 868; a release or acquire of
+// cluster scope at the buffers' barriers 1490 (it waits for every load in flight); packed additions 860 (a move and a half each, the products
+// arrive in registers that do not pair up); four warpgroups of 64 columns, scales four blocks ahead: no gain.
+// The 256 x 256 form spills 164 bytes of stores and 80 of loads a thread; builds with 92 and 100, and with 68 and 52, were 2 % slower.
+// 5120 x 5120 with weights in L2: one row 7.8 us (26 MB at the copy rate 4.0), 64 rows 11, 512 rows 22, 1024 rows 40, 2048 rows 62: from 65 rows to
+// some thousands whole tiles leave SMs without work (512 rows: 40 tiles of a pair on 74 pairs; 1024: 320 of a CTA, two rounds and 24 more).
 #include "vc_attn_shared.cuh"
 #include "vc_layer.cuh"
 #include "vc_sm100.cuh"
@@ -568,6 +571,7 @@ vc_status resolve(const vc_linear_params* p, vc_linear_params* out, Plan* plan) 
   if (pl.items > INT32_MAX) return VC_ERR_UNSUPPORTED;
   pl.ldp = (r.N + 3) / 4 * 4ll;
   if (pl.splits > 1 && r.M * pl.ldp > 1ll << 40) return VC_ERR_UNSUPPORTED;      // (the parts' bytes stay far below 2^64)
+  // (The parts have their place also where a cluster joins them in shared memory: the size goes by the splits alone.)
   pl.total = 256 + (pl.splits > 1 ? (size_t)pl.splits * r.M * pl.ldp * 4 : 0);
   *out = r;
   *plan = pl;

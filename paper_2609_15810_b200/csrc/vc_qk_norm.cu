@@ -5,11 +5,13 @@
 // shared memory), loads and stores are 16 bytes, and a head's sum of squares is a shuffle within its lanes.  The norm over
 // a token keeps the thread's part of the token in registers between the sum and the rotation: one pass over memory.
 //
-// 32760 tokens of d128, interleaved, 40 + 40 / 12 + 12 heads: rotation alone 213 / 66 us (97 / 94 % of the measured copy rate), with the norm per head
-// 229 / 85, per token 253 / 92 (1342 / 403 MB; a CTA's loads stand still while a token's sum is formed, and the angles cost 14 to 19).  Eight
+// 32760 tokens of d128, interleaved, 40 + 40 / 12 + 12 heads, calls that follow one another: rotation alone 213 / 66 us (97 / 94 % of the measured copy rate),
+// with the norm per head 229-236 / 85, per token 253-256 / 92 (1342 / 403 MB; a CTA's loads stand still while a token's sum is formed, and the angles cost 14 to 19).  Eight
 // channels a thread instead of 16: 302 for 260 at that time (angles, addresses and shuffles per row cost twice as much); CTAs of 256 threads: 282 (more
 // warps wait for a token's slowest); five or six CTAs an SM: 284 and 326 (spills), with three heads a thread 12 heads 98 for 105, 40 heads 333.
-// Halves with axes that are not multiples of 16 channels: 263 us for 24 + 24 heads (floor 124), the change of places in shared memory bounds it.
+// Halves whose axes are multiples of 16 channels: 24 + 24 heads with the norm per head 153 us (floor 124).  Other axes, the default split of d 64 and 128 among
+// them: 24 + 24 heads 262, 40 + 40 heads 420 (floor 206); the change of places in shared memory bounds it, head after head.  Under the token norm
+// the 16-bit form of these spills 64 bytes of stores and 32 of loads a thread.
 #include <cmath>
 
 #include "vc_layer.cuh"
